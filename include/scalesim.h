@@ -428,6 +428,161 @@ ss_status ss_interaction_distances_static(const int32_t* pos_xy, const uint32_t*
                                           uint32_t n_agents, uint32_t velocity, uint32_t radius,
                                           uint32_t* out, void* stream);
 
+/* ---- What a model does with resident units ---------------------------------
+ *
+ * Operators over a pool's units, found through its block table: they write
+ * tokens into an agent's KV pages, read them back, attend over them and apply
+ * its low-rank adapter, where the units are.  All work is queued on `stream`
+ * (a hipStream_t, NULL = the null stream) and the calls return without
+ * waiting, allocate nothing and may be captured into a graph.  Every array
+ * is device memory of the current device, owned by the caller, and stays as it
+ * is until the work has run; the structs themselves are host memory, read
+ * during the call.  Calls whose work can overlap need workspaces of their own.
+ *
+ * The host checks what it can see (pointers, sizes, strides): SS_ERR_ARG, and
+ * nothing is queued.  Values in device arrays are not checked: where they break
+ * the rules below, results are unspecified but no access goes outside the
+ * arrays, and every kernel ends.  SS_ERR_HIP if a launch fails. */
+#define SS_BF16 1u
+#define SS_F16  2u
+#define SS_E4M3 3u                  /* float8 e4m3 (finite, +-448) with float scales   */
+
+/* One layer's keys and values in a pool's units.  A unit's chunk holds a page
+ * of page_tokens tokens: element (token t, head h, i) lies at
+ *     k + unit * k_unit_bytes + t * token_bytes + h * head_bytes + i * size
+ * (v alike), so a page may hold head after head or token after token.  With
+ * SS_E4M3 the stored value is code * scale, the scale of (head h, token t) being
+ * the float at k + unit * k_unit_bytes + scale_off + 4 * (h * page_tokens + t).
+ * Logical unit j of an agent holds its tokens from j * page_tokens on. */
+typedef struct {
+    const int32_t*  units;          /* block table as ss_block_table gives it: agent a's  */
+    const uint64_t* agent_off;      /* logical unit j is units[agent_off[a] + j], -1 = away
+                                       (ids outside [0, capacity_units) count as away)    */
+    uint32_t n_agents;
+    uint32_t page_tokens;           /* power of two, 1 .. 1024                            */
+    uint64_t n_entries;             /* entries of `units` (sum of agent_units)            */
+    uint64_t capacity_units;        /* >= 1                                               */
+    void*    k;                     /* plane base of the layer's keys, 16-byte aligned;   */
+    void*    v;                     /* of its values.  Chunks with several layers: plane
+                                       base + the layer's offset inside the chunk         */
+    uint64_t k_unit_bytes;          /* bytes from unit to unit (chunk_bytes of the plane), */
+    uint64_t v_unit_bytes;          /* multiples of 16                                    */
+    uint32_t n_heads;               /* key/value heads, 1 .. 1024                         */
+    uint32_t head_dim;              /* multiple of 16, 16 .. 256                          */
+    uint32_t type;                  /* SS_BF16, SS_F16, SS_E4M3                           */
+    uint32_t pad;
+    uint64_t token_bytes;           /* multiples of 16; rows of a page do not overlap     */
+    uint64_t head_bytes;
+    uint64_t scale_off;             /* SS_E4M3: multiple of 16, behind the page's codes   */
+} ss_kv_cache;
+
+/* A ragged batch.  Request r has rows row_off[r] .. row_off[r+1] (new tokens)
+ * of agent agents[r].  Groups of consecutive requests may share a prefix, the
+ * first prefix_lens[g] tokens of another agent's units (a shared object in the
+ * same block table).  Rows behind row_off[n_requests] belong to no request and
+ * are neither read nor written. */
+typedef struct {
+    uint32_t n_rows;                /* rows of the row arrays, < 2^31                     */
+    uint32_t n_requests;            /* < 2^20                                             */
+    const uint32_t* row_off;        /* [n_requests + 1] nondecreasing, from 0, <= n_rows  */
+    const uint32_t* agents;         /* [n_requests]; ids >= n_agents: the agent is away   */
+    const uint32_t* lens;           /* [n_requests] tokens of the agent after this step,
+                                       the request's rows being the last of them: row i of
+                                       n holds token lens[r] - n + i.  (Not used by
+                                       ss_adapter_add.)                                   */
+    uint32_t n_groups;              /* 0 = no prefixes; < 2^20                            */
+    uint32_t pad;
+    const uint32_t* group_off;      /* [n_groups + 1] nondecreasing, <= n_requests: group g
+                                       is requests group_off[g] .. group_off[g+1]         */
+    const uint32_t* prefix_agents;  /* [n_groups]                                         */
+    const uint32_t* prefix_lens;    /* [n_groups] tokens                                  */
+} ss_batch;
+
+/* Write the rows' keys and values into their agents' pages.  k and v are
+ * [n_rows] rows of [n_heads][head_dim] SS_BF16 or SS_F16 values (`type`),
+ * row_stride and head_stride elements apart (multiples of 8; 16-byte aligned).
+ * A 16-bit cache has to have the rows' type and takes them as they are.  With
+ * SS_E4M3 each (row, head) gets the scale
+ *     s = max(largest finite |x| / 448, 2^-126)
+ * and the codes x / s, rounded to nearest even; infinities become the largest
+ * code, NaN stays NaN.  Rows whose unit is away or whose token is negative are
+ * not written.  Two rows for one token: either may be the one that is kept. */
+ss_status ss_kv_write(const ss_kv_cache* cache, const ss_batch* batch, const void* k,
+                      const void* v, uint32_t type, uint64_t row_stride, uint64_t head_stride,
+                      void* stream);
+
+/* The way back: row i of request r receives token lens[r] - n + i of its agent,
+ * rounded to `type` where the cache is SS_E4M3 (else `type` is the cache's).
+ * Rows whose unit is away or whose token is negative receive zeros. */
+ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, void* v,
+                     uint32_t type, uint64_t row_stride, uint64_t head_stride, void* stream);
+
+/* Attention of a batch over its agents' pages.  Query head h of n_q_heads (a
+ * multiple of n_heads) reads key/value head h / (n_q_heads / n_heads).  Row i of
+ * a request of n rows sees the whole prefix of its group, if it has one, and its
+ * agent's tokens 0 .. lens[r] - n + i (write the step's keys and values first):
+ *     out = sum_c softmax_c(scale q . k_c) v_c,   lse = ln sum_c exp(scale q . k_c)
+ * Tokens in units that are away are not seen; a row that sees nothing gets
+ * out = 0 and lse = -infinity.  A prefix of several requests is read once for
+ * many of them.  Keys and values that are not seen by any row of a request may
+ * hold anything, NaN included; an infinite or NaN value that only the later rows
+ * of a request see leaves its earlier rows of the same call unspecified.
+ *   q, out     [n_rows][n_q_heads][head_dim] SS_BF16 or SS_F16 (`type`; the
+ *              cache's unless that is SS_E4M3), strides in elements (multiples
+ *              of 8), 16-byte aligned; out must not overlap q;
+ *   lse        [n_rows][n_q_heads] floats, or NULL;
+ *   scale      finite (1 / sqrt(head_dim) as a rule);
+ *   workspace  ss_prefix_attention_workspace(...) bytes (a bound over all
+ *              lengths, 0 for arguments that the call refuses), 16-byte
+ *              aligned, no initialisation needed.
+ * Scores, softmax statistics and sums are held in 32 bits; the weights are
+ * rounded to 16 bits for the product with the values. */
+uint64_t ss_prefix_attention_workspace(const ss_kv_cache* cache, const ss_batch* batch,
+                                       uint32_t n_q_heads);
+ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, const void* q,
+                              void* out, float* lse, uint32_t type, uint32_t n_q_heads,
+                              uint64_t q_row_stride, uint64_t q_head_stride,
+                              uint64_t out_row_stride, uint64_t out_head_stride, float scale,
+                              void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* One projection of the adapters in a pool's units: for the agent whose logical
+ * unit `unit` is u, A is [rank][n_in] at a + u * a_unit_bytes and B [n_out][rank]
+ * at b + u * b_unit_bytes, both contiguous.  An adapter of a smaller rank fills
+ * up with zeros. */
+typedef struct {
+    const int32_t*  units;          /* block table, as in ss_kv_cache                     */
+    const uint64_t* agent_off;
+    uint32_t n_agents;
+    uint32_t unit;                  /* which of an agent's logical units (0 where it has one) */
+    uint64_t n_entries;
+    uint64_t capacity_units;
+    const void* a;                  /* 16-byte aligned plane base (+ offset in the chunk) */
+    const void* b;
+    uint64_t a_unit_bytes;          /* multiples of 16 below 2^31                         */
+    uint64_t b_unit_bytes;
+    uint32_t rank;                  /* multiple of 8, 8 .. 128                            */
+    uint32_t n_in, n_out;           /* multiples of 8, < 2^24                             */
+    uint32_t type;                  /* SS_BF16 or SS_F16                                  */
+} ss_adapters;
+
+/* out[t] = base[t] + s_r * B (A x[t]) for the rows t of each request r, with the
+ * adapter of agents[r] and s_r = scales[r] (NULL: 1): the agents' adapters beside
+ * the projection they share, whose output is `base`.  Rows of agents that are
+ * away, or have no such unit, get out = base.
+ *   x [n_rows][n_in], base and out [n_rows][n_out], of the adapters' type, row
+ *   strides in elements (multiples of 8), 16-byte aligned.  out may be base
+ *   (same address and stride), and must not overlap x or otherwise base;
+ *   scales     [n_requests] floats or NULL;
+ *   workspace  ss_adapter_add_workspace(...) bytes, 16-byte aligned, no
+ *              initialisation needed.
+ * A x is summed and kept in 32 bits (as two 16-bit parts in the second product). */
+uint64_t ss_adapter_add_workspace(const ss_adapters* adapters, uint32_t n_rows,
+                                  uint32_t n_requests);
+ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, const void* x,
+                         const void* base, void* out, uint64_t x_stride, uint64_t base_stride,
+                         uint64_t out_stride, const float* scales, void* workspace,
+                         uint64_t workspace_bytes, void* stream);
+
 /* ---- Load-task scheduler (Appendix A, "Load task scheduler" and
  * "Preemption support") ------------------------------------------------------
  *

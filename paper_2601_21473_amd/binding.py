@@ -41,7 +41,11 @@ EXPORTS = ["ss_pool_create", "ss_pool_destroy", "ss_plan_step", "ss_evict_pack",
            "ss_event_destroy", "ss_event_record", "ss_event_elapsed", "ss_loader_create",
            "ss_loader_destroy", "ss_loader_submit", "ss_loader_pump", "ss_loader_pending",
            "ss_loader_sync", "ss_loader_get_stats", "ss_debug_fail_copy",
-           "ss_interaction_distances_static", "ss_probe_hop_distances"]
+           "ss_interaction_distances_static", "ss_probe_hop_distances", "ss_kv_write", "ss_kv_read",
+           "ss_prefix_attention_workspace", "ss_prefix_attention", "ss_adapter_add_workspace",
+           "ss_adapter_add"]
+
+SS_BF16, SS_F16, SS_E4M3 = 1, 2, 3
 
 
 class ss_load_task(C.Structure):
@@ -94,6 +98,31 @@ class ss_stats(C.Structure):
                 ("direct_out_ms", C.c_double), ("direct_in_ms", C.c_double),
                 ("plan_enqueue_us", C.c_double * 4), ("duplex_launches", C.c_uint64),
                 ("duplex_bytes", C.c_uint64), ("duplex_ms", C.c_double)]
+
+
+class ss_kv_cache(C.Structure):
+    _fields_ = [("units", C.c_void_p), ("agent_off", C.c_void_p), ("n_agents", C.c_uint32),
+                ("page_tokens", C.c_uint32), ("n_entries", C.c_uint64),
+                ("capacity_units", C.c_uint64), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_unit_bytes", C.c_uint64), ("v_unit_bytes", C.c_uint64),
+                ("n_heads", C.c_uint32), ("head_dim", C.c_uint32), ("type", C.c_uint32),
+                ("pad", C.c_uint32), ("token_bytes", C.c_uint64), ("head_bytes", C.c_uint64),
+                ("scale_off", C.c_uint64)]
+
+
+class ss_batch(C.Structure):
+    _fields_ = [("n_rows", C.c_uint32), ("n_requests", C.c_uint32), ("row_off", C.c_void_p),
+                ("agents", C.c_void_p), ("lens", C.c_void_p), ("n_groups", C.c_uint32),
+                ("pad", C.c_uint32), ("group_off", C.c_void_p), ("prefix_agents", C.c_void_p),
+                ("prefix_lens", C.c_void_p)]
+
+
+class ss_adapters(C.Structure):
+    _fields_ = [("units", C.c_void_p), ("agent_off", C.c_void_p), ("n_agents", C.c_uint32),
+                ("unit", C.c_uint32), ("n_entries", C.c_uint64), ("capacity_units", C.c_uint64),
+                ("a", C.c_void_p), ("b", C.c_void_p), ("a_unit_bytes", C.c_uint64),
+                ("b_unit_bytes", C.c_uint64), ("rank", C.c_uint32), ("n_in", C.c_uint32),
+                ("n_out", C.c_uint32), ("type", C.c_uint32)]
 
 
 class ScaleSimError(RuntimeError):
@@ -175,6 +204,14 @@ def load():
         "ss_interaction_distances_workspace": ([C.c_uint32], C.c_uint64),
         "ss_interaction_distances": ([P, P, C.c_uint32, C.c_uint32, C.c_uint32, P, P, C.c_uint64,
                                       P], C.c_int32),
+        "ss_kv_write": ([P, P, P, P, C.c_uint32, C.c_uint64, C.c_uint64, P], C.c_int32),
+        "ss_kv_read": ([P, P, P, P, C.c_uint32, C.c_uint64, C.c_uint64, P], C.c_int32),
+        "ss_prefix_attention_workspace": ([P, P, C.c_uint32], C.c_uint64),
+        "ss_prefix_attention": ([P, P, P, P, P, C.c_uint32, C.c_uint32, C.c_uint64, C.c_uint64,
+                                 C.c_uint64, C.c_uint64, C.c_float, P, C.c_uint64, P], C.c_int32),
+        "ss_adapter_add_workspace": ([P, C.c_uint32, C.c_uint32], C.c_uint64),
+        "ss_adapter_add": ([P, P, P, P, P, C.c_uint64, C.c_uint64, C.c_uint64, P, P, C.c_uint64, P],
+                           C.c_int32),
     }
     for name, (args, res) in sig.items():
         f = getattr(L, name)
@@ -246,6 +283,8 @@ class Pool:
         _check(L.ss_pool_create(C.byref(d), C.byref(h)))
         self._h = h
         self.unit_bytes = int(self._chunk.sum())
+        self._capacity = int(capacity_units)
+        self._bases = [int(b) for b in plane_base]
         # reused argument structs of ss_plan_step
         self._prm, self._out = ss_plan_params(), ss_plan()
         self._prm_ref, self._out_ref = C.byref(self._prm), C.byref(self._out)
@@ -316,6 +355,45 @@ class Pool:
         u, o = C.c_void_p(), C.c_void_p()
         _check(load().ss_block_table(self._h, C.byref(u), C.byref(o)))
         return u.value, o.value
+
+    def _table(self) -> dict:
+        units, off = self.block_table()
+        return dict(units=units, agent_off=off, n_agents=self.n_agents,
+                    n_entries=int(self._units.sum(dtype=np.uint64)), capacity_units=self._capacity)
+
+    def kv_cache(self, k_plane: int, v_plane: int, *, page_tokens: int, n_heads: int, head_dim: int,
+                 type: int, order: str = "head", k_offset: int = 0, v_offset: int = 0,
+                 ) -> ss_kv_cache:
+        """The layer whose keys and values lie in planes ``k_plane`` and ``v_plane``
+        of the pool, ``k_offset`` and ``v_offset`` bytes into their chunks.  A page
+        holds head after head (``order="head"``) or token after token
+        (``"token"``), contiguous, with the scales of ``SS_E4M3`` right behind."""
+        row = head_dim * (1 if type == SS_E4M3 else 2)
+        by_head = {"head": True, "token": False}[order]
+        token, head = (row, page_tokens * row) if by_head else (n_heads * row, row)
+        body = n_heads * page_tokens * row
+        need = body + (4 * n_heads * page_tokens if type == SS_E4M3 else 0)
+        for plane, offset in ((k_plane, k_offset), (v_plane, v_offset)):
+            if offset < 0 or offset + need > int(self._chunk[plane]):
+                raise ValueError(f"a page of {need} bytes at {offset} does not fit into the "
+                                 f"{int(self._chunk[plane])}-byte chunks of plane {plane}")
+        return kv_cache(**self._table(), k=self._bases[k_plane] + k_offset,
+                        v=self._bases[v_plane] + v_offset, k_unit_bytes=self._chunk[k_plane],
+                        v_unit_bytes=self._chunk[v_plane], page_tokens=page_tokens,
+                        n_heads=n_heads, head_dim=head_dim, type=type, token_bytes=token,
+                        head_bytes=head, scale_off=body if type == SS_E4M3 else 0)
+
+    def adapters(self, a_plane: int, b_plane: int, *, rank: int, n_in: int, n_out: int, type: int,
+                 unit: int = 0, a_offset: int = 0, b_offset: int = 0) -> ss_adapters:
+        """The projection whose A and B lie in planes ``a_plane`` and ``b_plane``."""
+        for plane, offset, n in ((a_plane, a_offset, n_in), (b_plane, b_offset, n_out)):
+            if offset < 0 or offset + 2 * rank * n > int(self._chunk[plane]):
+                raise ValueError(f"a matrix of {2 * rank * n} bytes at {offset} does not fit into "
+                                 f"the {int(self._chunk[plane])}-byte chunks of plane {plane}")
+        return adapters(**self._table(), a=self._bases[a_plane] + a_offset,
+                        b=self._bases[b_plane] + b_offset, a_unit_bytes=self._chunk[a_plane],
+                        b_unit_bytes=self._chunk[b_plane], rank=rank, n_in=n_in, n_out=n_out,
+                        type=type, unit=unit)
 
     def block_table_host(self, agent: int) -> np.ndarray:
         cap = int(self._units[agent])
@@ -494,6 +572,76 @@ def interaction_distances_static(pos_xy: int, d_action: int, n_agents: int, velo
     _check(load().ss_interaction_distances_static(int(pos_xy), int(d_action), int(n_agents),
                                                   int(velocity), int(radius), int(out),
                                                   int(stream)))
+
+
+# ---- what a model does with resident units ------------------------------------
+
+def kv_cache(*, units, agent_off, n_agents, n_entries, capacity_units, k, v, k_unit_bytes,
+             v_unit_bytes, page_tokens, n_heads, head_dim, type, token_bytes, head_bytes,
+             scale_off=0) -> ss_kv_cache:
+    """One layer's keys and values in a pool's units (device addresses)."""
+    return ss_kv_cache(int(units), int(agent_off), int(n_agents), int(page_tokens), int(n_entries),
+                       int(capacity_units), int(k), int(v), int(k_unit_bytes), int(v_unit_bytes),
+                       int(n_heads), int(head_dim), int(type), 0, int(token_bytes), int(head_bytes),
+                       int(scale_off))
+
+
+def batch(*, n_rows, n_requests, row_off, agents, lens=0, n_groups=0, group_off=0,
+          prefix_agents=0, prefix_lens=0) -> ss_batch:
+    """A ragged batch (device addresses)."""
+    return ss_batch(int(n_rows), int(n_requests), int(row_off), int(agents), int(lens),
+                    int(n_groups), 0, int(group_off), int(prefix_agents), int(prefix_lens))
+
+
+def adapters(*, units, agent_off, n_agents, n_entries, capacity_units, a, b, a_unit_bytes,
+             b_unit_bytes, rank, n_in, n_out, type, unit=0) -> ss_adapters:
+    """One projection of the adapters in a pool's units (device addresses)."""
+    return ss_adapters(int(units), int(agent_off), int(n_agents), int(unit), int(n_entries),
+                       int(capacity_units), int(a), int(b), int(a_unit_bytes), int(b_unit_bytes),
+                       int(rank), int(n_in), int(n_out), int(type))
+
+
+def kv_write(cache: ss_kv_cache, batch: ss_batch, k: int, v: int, *, type: int, strides,
+             stream: int = 0):
+    """Queue ``ss_kv_write``; ``strides`` = (row, head) in elements."""
+    _check(load().ss_kv_write(C.byref(cache), C.byref(batch), int(k), int(v), int(type),
+                              int(strides[0]), int(strides[1]), int(stream) or None))
+
+
+def kv_read(cache: ss_kv_cache, batch: ss_batch, k: int, v: int, *, type: int, strides,
+            stream: int = 0):
+    """Queue ``ss_kv_read``; ``strides`` = (row, head) in elements."""
+    _check(load().ss_kv_read(C.byref(cache), C.byref(batch), int(k), int(v), int(type),
+                             int(strides[0]), int(strides[1]), int(stream) or None))
+
+
+def prefix_attention_workspace(cache: ss_kv_cache, batch: ss_batch, n_q_heads: int) -> int:
+    return int(load().ss_prefix_attention_workspace(C.byref(cache), C.byref(batch), int(n_q_heads)))
+
+
+def prefix_attention(cache: ss_kv_cache, batch: ss_batch, q: int, out: int, *, type: int,
+                     n_q_heads: int, q_strides, out_strides, scale: float, workspace: int,
+                     workspace_bytes: int, lse: int = 0, stream: int = 0):
+    """Queue ``ss_prefix_attention``; strides = (row, head) in elements."""
+    _check(load().ss_prefix_attention(C.byref(cache), C.byref(batch), int(q), int(out),
+                                      int(lse) or None, int(type), int(n_q_heads),
+                                      int(q_strides[0]), int(q_strides[1]), int(out_strides[0]),
+                                      int(out_strides[1]), float(scale), int(workspace),
+                                      int(workspace_bytes), int(stream) or None))
+
+
+def adapter_add_workspace(adapters: ss_adapters, n_rows: int, n_requests: int) -> int:
+    return int(load().ss_adapter_add_workspace(C.byref(adapters), int(n_rows), int(n_requests)))
+
+
+def adapter_add(adapters: ss_adapters, batch: ss_batch, x: int, base: int, out: int, *,
+                x_stride: int, base_stride: int, out_stride: int, workspace: int,
+                workspace_bytes: int, scales: int = 0, stream: int = 0):
+    """Queue ``ss_adapter_add``; row strides in elements."""
+    _check(load().ss_adapter_add(C.byref(adapters), C.byref(batch), int(x), int(base), int(out),
+                                 int(x_stride), int(base_stride), int(out_stride),
+                                 int(scales) or None, int(workspace), int(workspace_bytes),
+                                 int(stream) or None))
 
 
 class Stream:

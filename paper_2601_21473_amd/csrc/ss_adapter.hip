@@ -1,0 +1,371 @@
+// Low-rank adapters of many requests beside a shared projection (ss_adapter_add):
+//     out[t] = base[t] + s_r B_a (A_a x[t])
+// for the rows t of each request r, with its agent's A [rank][n_in] and
+// B [n_out][rank] where the pool keeps them.
+//
+// Two kernels.  k_adapter_in computes A x in tiles of up to 16 rows of one request,
+// the sum over n_in cut into pieces so that few rows still fill the card; the
+// pieces go to the workspace in 32 bits and k_adapter_out adds them up, in the same
+// order every time, when it loads them.  Both are matrix products of 16 x 16 x 32
+// whose operands are rows contiguous along the summed index, so lanes load them
+// from memory in the layout the instruction wants.
+#include <algorithm>
+#include <type_traits>
+
+#include "ss_model.h"
+
+namespace ss {
+
+namespace {
+
+constexpr int kTile = 16;               // rows of a tile
+constexpr int kThreads = 256;
+constexpr int kOutCols = 256;           // columns of out per workgroup
+
+struct AdapterArgs {
+    Table tab;
+    const char* a;
+    const char* b;
+    u64 a_unit, b_unit;
+    unsigned unit, rank, n_in, n_out;
+    const char* x;
+    const char* base;
+    char* out;
+    u64 x_row, base_row, out_row;       // bytes
+    const float* scales;
+    const unsigned* row_off;
+    const unsigned* agents;
+    unsigned n_rows, n_requests;
+    float* low;                         // [pieces][n_rows][rank]: parts of A x
+    unsigned pieces, piece;             // pieces of n_in, and elements of one
+};
+
+// Tile i of the batch: request r's tiles begin at row_off[r] / 16 + r, which leaves
+// room for every request's last, partly filled tile without a pass over the offsets.
+// Returns the tile's rows (0: no such tile).
+__device__ inline unsigned tile_of(const AdapterArgs& A, unsigned i, unsigned* r, unsigned* row0) {
+    *r = wave_search(A.n_requests, i, [&](unsigned j) {
+        const u64 s = (u64)A.row_off[j] / kTile + j;
+        return (unsigned)(s < 0xffffffffu ? s : 0xffffffffu);
+    });
+    const unsigned b = A.row_off[*r], rows = request_rows(A.row_off, *r, A.n_rows);
+    const u64 first = (u64)b / kTile + *r;
+    if (i < first) return 0;
+    const u64 at = ((u64)i - first) * kTile;
+    if (at >= rows) return 0;
+    *row0 = b + (unsigned)at;
+    return rows - at < kTile ? rows - (unsigned)at : kTile;
+}
+
+__device__ inline int adapter_of(const AdapterArgs& A, unsigned r) {
+    u64 first;
+    const unsigned n = A.tab.row(A.agents[r], &first);
+    return A.unit < n ? A.tab.unit(first + A.unit) : -1;
+}
+
+// A workgroup per tile and piece.  kTiles = rank / 16 (rounded up) products of 16 ranks x 16
+// rows; the four waves take 32 elements of the piece in turn.
+template <class T, int kTiles>
+__global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
+    __shared__ __align__(16) f32x4 s_acc[3][kTiles][64];
+    unsigned r, row0;
+    const unsigned rows = tile_of(A, blockIdx.x / A.pieces, &r, &row0), piece = blockIdx.x % A.pieces;
+    if (!rows) return;
+    const int unit = adapter_of(A, r);
+    if (unit < 0) return;
+    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const unsigned col = lane % 16, quad = lane / 16;
+    const unsigned k0 = piece * A.piece, k1 = min(A.n_in, k0 + A.piece);
+    const char* xr = A.x + (u64)(row0 + (col < rows ? col : 0)) * A.x_row;
+    const char* am = A.a + (u64)unit * A.a_unit;
+    const char* ar[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+        ar[t] = am + (u64)(t * 16 + col < A.rank ? t * 16 + col : 0) * A.n_in * 2;
+    f32x4 acc[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0, 0, 0, 0};
+    const u32x4 zero = {0, 0, 0, 0};
+    for (unsigned k = k0 + wave * 32; k < k1; k += 128) {
+        const unsigned at = k + quad * 8;
+        const bool in = at < k1;
+        const u64 off = (u64)(in ? at : k0) * 2;
+        u32x4 xf = *reinterpret_cast<const u32x4*>(xr + off);
+        if (!in || col >= rows) xf = zero;
+        u32x4 af[kTiles];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            af[t] = *reinterpret_cast<const u32x4*>(ar[t] + off);
+            if (!in || t * 16 + col >= A.rank) af[t] = zero;
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) acc[t] = T::mma(af[t], xf, acc[t]);
+    }
+    if (wave) {
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) s_acc[wave - 1][t][lane] = acc[t];
+    }
+    __syncthreads();
+    if (wave || col >= rows) return;
+    float* to = A.low + ((u64)piece * A.n_rows + row0 + col) * A.rank;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const f32x4 s = acc[t] + s_acc[0][t][lane] + s_acc[1][t][lane] + s_acc[2][t][lane];
+        const unsigned rr = t * 16 + quad * 4;
+        if (rr < A.rank) *reinterpret_cast<f32x4*>(to + rr) = s;
+    }
+}
+
+// A workgroup per tile and kOutCols columns.  A x enters as two 16-bit parts, the rounded value and
+// what the rounding left, next to each other along the summed index (the columns of
+// B are read for both), so that its 32 bits count for 16 (bf16) or 22 (fp16) of
+// them.  For fp16 each row is first divided by a power of two near its largest
+// value, as sums can pass that type's range.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_adapter_out(AdapterArgs A) {
+    __shared__ __align__(16) unsigned short s_h[kTile][2 * 128 + 8];    // two parts, zeros behind
+    __shared__ float s_scale[kTile];
+    __shared__ __align__(16) float s_y[kTile][kOutCols + 4];
+    unsigned r, row0;
+    const unsigned parts = (A.n_out + kOutCols - 1) / kOutCols;
+    const unsigned rows = tile_of(A, blockIdx.x / parts, &r, &row0);
+    if (!rows) return;
+    const int unit = adapter_of(A, r);
+    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const unsigned col = lane % 16, quad = lane / 16;
+    const unsigned n0 = blockIdx.x % parts * kOutCols;
+    const unsigned slots = (2 * A.rank + 31) & ~31u;
+    if (unit >= 0) {
+        // 16 lanes a row: eight ranks each
+        const unsigned i = threadIdx.x / 16, c = threadIdx.x % 16 * 8;
+        float h[8], top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = 0.f;
+        if (i < rows && c < A.rank)
+            for (unsigned p = 0; p < A.pieces; ++p) {
+                const float* from = A.low + ((u64)p * A.n_rows + row0 + i) * A.rank + c;
+                const f32x4 u = *reinterpret_cast<const f32x4*>(from);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(from + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    h[j] += u[j];
+                    h[4 + j] += v[j];
+                }
+            }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(h[j]));
+#pragma unroll
+        for (int m = 8; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+        float unscale = 1.f;
+        if constexpr (std::is_same<T, F16>::value) {
+            if (top > 0.f && top < INFINITY) {
+                const int e = min(max(ilogbf(top), -100), 100);
+                unscale = ldexpf(1.f, e);
+                const float s = ldexpf(1.f, -e);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[j] *= s;
+            }
+        }
+        if (c == 0) s_scale[i] = unscale * (A.scales ? A.scales[r] : 1.f);
+        // columns 0 .. rank: rounded values, rank .. 2 rank: the rests, then zeros
+        unsigned hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            hi[j] = T::pack(h[2 * j], h[2 * j + 1]);
+            const float a = T::lo(hi[j]), b = T::hi(hi[j]);         // no rest of an infinity
+            lo[j] = T::pack(fabsf(a) < INFINITY ? h[2 * j] - a : 0.f,
+                            fabsf(b) < INFINITY ? h[2 * j + 1] - b : 0.f);
+        }
+        if (c < A.rank) {
+            *reinterpret_cast<u32x4*>(&s_h[i][c]) = u32x4{hi[0], hi[1], hi[2], hi[3]};
+            *reinterpret_cast<u32x4*>(&s_h[i][A.rank + c]) = u32x4{lo[0], lo[1], lo[2], lo[3]};
+        }
+        if (2 * A.rank + c < slots)
+            *reinterpret_cast<u32x4*>(&s_h[i][2 * A.rank + c]) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        // products of 16 columns x 16 rows, four to a wave
+        f32x4 acc[4];
+        const char* br[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            acc[t] = f32x4{0, 0, 0, 0};
+            const unsigned n = n0 + wave * 64 + t * 16 + col;
+            br[t] = A.b + (u64)unit * A.b_unit + (u64)(n < A.n_out ? n : 0) * A.rank * 2;
+        }
+        for (unsigned k = 0; k < slots; k += 32) {
+            const unsigned at = k + quad * 8;           // a slot of eight
+            const unsigned from = at < A.rank ? at : at - A.rank;
+            const u32x4 hf = *reinterpret_cast<const u32x4*>(&s_h[col][at]);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                u32x4 bf = {0, 0, 0, 0};
+                if (at < 2 * A.rank) bf = *reinterpret_cast<const u32x4*>(br[t] + from * 2);
+                acc[t] = T::mma(bf, hf, acc[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            *reinterpret_cast<f32x4*>(&s_y[col][wave * 64 + t * 16 + quad * 4]) = acc[t];
+        __syncthreads();
+    } else if (A.base == A.out) {
+        return;
+    }
+    for (unsigned e = threadIdx.x; e < rows * (kOutCols / 8); e += kThreads) {
+        const unsigned i = e / (kOutCols / 8), c = e % (kOutCols / 8) * 8;
+        if (n0 + c >= A.n_out) continue;
+        const u64 at = (u64)(n0 + c) * 2;
+        u32x4 w = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + i) * A.base_row + at);
+        if (unit >= 0) {
+            const float s = s_scale[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[j] = T::pack(T::lo(w[j]) + s * s_y[i][c + 2 * j], T::hi(w[j]) + s * s_y[i][c + 2 * j + 1]);
+        }
+        *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + i) * A.out_row + at) = w;
+    }
+}
+
+template <class T>
+void adapter_launch(const AdapterArgs& A, hipStream_t st) {
+    const unsigned tiles = A.n_rows / kTile + A.n_requests;
+    const dim3 in(A.pieces * tiles), out((A.n_out + kOutCols - 1) / kOutCols * tiles), block(kThreads);
+    switch ((A.rank + 15) / 16) {
+        case 1: hipLaunchKernelGGL((k_adapter_in<T, 1>), in, block, 0, st, A); break;
+        case 2: hipLaunchKernelGGL((k_adapter_in<T, 2>), in, block, 0, st, A); break;
+        case 3:
+        case 4: hipLaunchKernelGGL((k_adapter_in<T, 4>), in, block, 0, st, A); break;
+        default: hipLaunchKernelGGL((k_adapter_in<T, 8>), in, block, 0, st, A); break;
+    }
+    hipLaunchKernelGGL((k_adapter_out<T>), out, block, 0, st, A);
+}
+
+// n_in is cut into pieces of at least 256 elements (two rounds of the four waves)
+// until about 1,024 workgroups run, four a compute unit.
+void pieces_of(u64 n_rows, u64 n_requests, u64 n_in, unsigned* pieces, unsigned* piece) {
+    const u64 tiles = n_rows / kTile + n_requests;
+    const u64 want = std::max<u64>(1, std::min<u64>((1024 + tiles - 1) / tiles, (n_in + 255) / 256));
+    const u64 len = ((n_in + want - 1) / want + 127) / 128 * 128;
+    *piece = (unsigned)len;
+    *pieces = (unsigned)((n_in + len - 1) / len);
+}
+
+ss_status adapter_args(const ss_adapters* a) {
+    if (!a) return set_err(SS_ERR_ARG, "adapters is NULL");
+    const ss_status s = table_args(a->units, a->agent_off, a->n_agents, a->n_entries, a->capacity_units);
+    if (s != SS_OK) return s;
+    if (!a->a || !a->b || ((reinterpret_cast<uintptr_t>(a->a) | reinterpret_cast<uintptr_t>(a->b)) & 15))
+        return set_err(SS_ERR_ARG, "adapters a and b must be 16-byte aligned pointers");
+    if (a->rank < 8 || a->rank > 128 || a->rank % 8)
+        return set_err(SS_ERR_ARG, "rank must be a multiple of 8 in [8, 128]");
+    for (u64 n : {a->n_in, a->n_out})
+        if (n < 8 || n % 8 || n >= (1u << 24))
+            return set_err(SS_ERR_ARG, "n_in and n_out must be multiples of 8 in [8, 2^24)");
+    if (a->type != SS_BF16 && a->type != SS_F16)
+        return set_err(SS_ERR_ARG, "adapters must be SS_BF16 or SS_F16, not type %u", a->type);
+    if (a->a_unit_bytes % 16 || a->b_unit_bytes % 16 || a->a_unit_bytes >= (1ull << 31) ||
+        a->b_unit_bytes >= (1ull << 31))
+        return set_err(SS_ERR_ARG, "adapter byte distances must be multiples of 16 below 2^31");
+    if (a->capacity_units > 1 && (a->a_unit_bytes < 2ull * a->rank * a->n_in ||
+                                  a->b_unit_bytes < 2ull * a->rank * a->n_out))
+        return set_err(SS_ERR_ARG, "a matrix does not fit into a unit's chunk");
+    return SS_OK;
+}
+
+}  // namespace
+
+}  // namespace ss
+
+using namespace ss;
+
+extern "C" {
+
+uint64_t ss_adapter_add_workspace(const ss_adapters* adapters, uint32_t n_rows, uint32_t n_requests) {
+    if (adapter_args(adapters) != SS_OK || n_rows == 0 || n_requests == 0 || n_rows >= (1u << 31) ||
+        n_requests >= (1u << 20))
+        return 0;
+    unsigned pieces, piece;
+    pieces_of(n_rows, n_requests, adapters->n_in, &pieces, &piece);
+    return (uint64_t)pieces * n_rows * adapters->rank * 4;
+}
+
+ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, const void* x,
+                         const void* base, void* out, uint64_t x_stride, uint64_t base_stride,
+                         uint64_t out_stride, const float* scales, void* workspace,
+                         uint64_t workspace_bytes, void* stream) {
+    ss_status s = adapter_args(adapters);
+    if (s == SS_OK) s = batch_args(batch, false, false);
+    if (s != SS_OK) return s;
+    const u64 rows = batch->n_rows;
+    if (rows == 0 || batch->n_requests == 0) return SS_OK;
+    const unsigned n_in = adapters->n_in, n_out = adapters->n_out;
+    if ((s = rows_args("x", x, rows, 1, n_in, x_stride, n_in, false)) != SS_OK ||
+        (s = rows_args("base", base, rows, 1, n_out, base_stride, n_out, false)) != SS_OK ||
+        (s = rows_args("out", out, rows, 1, n_out, out_stride, n_out, true)) != SS_OK)
+        return s;
+    if ((rows / kTile + batch->n_requests) * ((n_out + kOutCols - 1) / kOutCols) >= (1ull << 31))
+        return set_err(SS_ERR_ARG, "n_rows * n_out is too large");
+    const u64 x_bytes = rows_bytes(rows, 1, n_in, x_stride, 0);
+    const u64 base_bytes = rows_bytes(rows, 1, n_out, base_stride, 0);
+    const u64 out_bytes = rows_bytes(rows, 1, n_out, out_stride, 0);
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(x), b0 = reinterpret_cast<uintptr_t>(base);
+    const uintptr_t o0 = reinterpret_cast<uintptr_t>(out);
+    if (x0 < o0 + out_bytes && o0 < x0 + x_bytes) return set_err(SS_ERR_ARG, "out overlaps x");
+    if (!(b0 == o0 && base_stride == out_stride) && b0 < o0 + out_bytes && o0 < b0 + base_bytes)
+        return set_err(SS_ERR_ARG, "out overlaps base without being it");
+    const u64 need = ss_adapter_add_workspace(adapters, batch->n_rows, batch->n_requests);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
+        return set_err(SS_ERR_ARG, "workspace must be a 16-byte aligned pointer");
+    if (workspace_bytes < need)
+        return set_err(SS_ERR_ARG, "workspace_bytes %llu < %llu", (unsigned long long)workspace_bytes,
+                       (unsigned long long)need);
+    int dev = -1;
+    if ((s = current_device(&dev)) != SS_OK ||
+        (s = table_memory(adapters->units, adapters->agent_off, adapters->n_agents, adapters->n_entries,
+                          dev)) != SS_OK ||
+        (s = batch_memory(batch, false, false, dev)) != SS_OK)
+        return s;
+    const u64 last = adapters->capacity_units - 1;
+    if (!device_range_ok(adapters->a, last * adapters->a_unit_bytes + 2ull * adapters->rank * n_in, dev))
+        return device_error("adapters a", dev);
+    if (!device_range_ok(adapters->b, last * adapters->b_unit_bytes + 2ull * adapters->rank * n_out, dev))
+        return device_error("adapters b", dev);
+    if (!device_range_ok(x, x_bytes, dev)) return device_error("x", dev);
+    if (!device_range_ok(base, base_bytes, dev)) return device_error("base", dev);
+    if (!device_range_ok(out, out_bytes, dev)) return device_error("out", dev);
+    if (scales && !device_range_ok(scales, (u64)batch->n_requests * 4, dev))
+        return device_error("scales", dev);
+    if (!device_range_ok(workspace, need, dev)) return device_error("workspace", dev);
+    AdapterArgs A{};
+    A.tab = table_of(adapters->units, adapters->agent_off, adapters->n_agents, adapters->n_entries,
+                     adapters->capacity_units);
+    A.a = static_cast<const char*>(adapters->a);
+    A.b = static_cast<const char*>(adapters->b);
+    A.a_unit = adapters->a_unit_bytes;
+    A.b_unit = adapters->b_unit_bytes;
+    A.unit = adapters->unit;
+    A.rank = adapters->rank;
+    A.n_in = n_in;
+    A.n_out = n_out;
+    A.x = static_cast<const char*>(x);
+    A.base = static_cast<const char*>(base);
+    A.out = static_cast<char*>(out);
+    A.x_row = 2 * x_stride;
+    A.base_row = 2 * base_stride;
+    A.out_row = 2 * out_stride;
+    A.scales = scales;
+    A.row_off = batch->row_off;
+    A.agents = batch->agents;
+    A.n_rows = batch->n_rows;
+    A.n_requests = batch->n_requests;
+    A.low = static_cast<float*>(workspace);
+    pieces_of(rows, batch->n_requests, n_in, &A.pieces, &A.piece);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (adapters->type == SS_BF16) adapter_launch<Bf16>(A, st);
+    else adapter_launch<F16>(A, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return set_err(SS_ERR_HIP, "adapter kernels: %s", hipGetErrorString(e));
+    return SS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,385 @@
+// Tokens into and out of a pool's KV pages (ss_kv_write, ss_kv_read), and the
+// argument checks of every operator over resident units.
+//
+// Both directions move each byte once and compute next to nothing, so HBM bounds
+// them and the layout follows the memory: 16 bytes a lane on the 16-bit side, a
+// head's row in 8, 16 or 32 consecutive lanes, so that the largest |x| of a row
+// needs 3 to 5 lane exchanges and no memory.
+#include <algorithm>
+#include <cmath>
+
+#include "ss_model.h"
+
+namespace ss {
+
+namespace {
+
+struct CacheArgs {
+    Table tab;
+    char* plane[2];                 // keys, values
+    u64 unit_bytes[2];
+    u64 token_bytes, head_bytes, scale_off;
+    char* rows[2];                  // 16-bit rows: read by a write, written by a read
+    u64 row_stride, head_stride;    // bytes
+    const unsigned* row_off;
+    const unsigned* agents;
+    const unsigned* lens;
+    unsigned n_rows, n_requests;
+    unsigned n_heads, dim;
+    unsigned shift;                 // page_tokens = 1 << shift
+    unsigned rows_per_block;        // 1, 2, 4, 8 or 16
+};
+
+constexpr int kCacheThreads = 256;
+
+// Where row t of the batch lies: its unit and token in the page, unit -1 if away
+// and -2 if no request has the row.  16 lanes search the requests together.
+__device__ inline int place_of(const CacheArgs& A, unsigned t, unsigned sub, unsigned* slot) {
+    unsigned lo = 0, n = A.n_requests;
+    const unsigned base = __lane_id() & ~15u;
+    while (n > 1) {                             // n is the same in the 16 lanes
+        const unsigned step = (n + 15) / 16;
+        const unsigned at = sub * step;
+        const bool p = at < n && A.row_off[lo + (at < n ? at : 0)] <= t;
+        const unsigned m = (unsigned)(__ballot(p) >> base) & 0xffffu;
+        const unsigned c = m ? 31u - (unsigned)__builtin_clz(m) : 0u;
+        lo += c * step;
+        n = n - c * step < step ? n - c * step : step;
+    }
+    const unsigned b = A.row_off[lo], rows = request_rows(A.row_off, lo, A.n_rows);
+    if (t >= A.n_rows || t < b || t - b >= rows) return -2;
+    const long long token = (long long)A.lens[lo] - rows + (t - b);
+    if (token < 0) return -1;
+    u64 first;
+    const unsigned pages = A.tab.row(A.agents[lo], &first);
+    const u64 page = (u64)token >> A.shift;
+    *slot = (unsigned)token & ((1u << A.shift) - 1u);
+    return page < pages ? A.tab.unit(first + page) : -1;
+}
+
+// One workgroup moves rows_per_block rows of keys and values.  kWrite: rows to
+// pages.  kLanes lanes hold a head's row, 8 values each (dim <= 8 kLanes).
+template <class T, bool kE4m3, bool kWrite, int kLanes>
+__global__ __launch_bounds__(kCacheThreads) void k_cache(CacheArgs A) {
+    __shared__ int s_unit[16];
+    __shared__ unsigned s_slot[16];
+    const unsigned row0 = blockIdx.x * A.rows_per_block;
+    {
+        const unsigned i = threadIdx.x / 16, sub = threadIdx.x % 16;
+        unsigned slot = 0;
+        const int u = place_of(A, row0 + i, sub, &slot);
+        if (sub == 0) {
+            s_unit[i] = u;
+            s_slot[i] = slot;
+        }
+    }
+    __syncthreads();
+    const unsigned per_row = 2 * A.n_heads;                 // head rows of keys and values
+    const unsigned d0 = (threadIdx.x % kLanes) * 8;
+    const bool in = d0 < A.dim;
+    for (unsigned g = threadIdx.x / kLanes; g < per_row * A.rows_per_block;
+         g += kCacheThreads / kLanes) {
+        const unsigned i = g / per_row, wh = g % per_row;
+        const int unit = s_unit[i];
+        if (unit < (kWrite ? 0 : -1)) continue;
+        const unsigned what = wh >= A.n_heads, h = wh - (what ? A.n_heads : 0);
+        char* row = A.rows[what] + (u64)(row0 + i) * A.row_stride + (u64)h * A.head_stride + d0 * 2;
+        const unsigned slot = s_slot[i];
+        char* base = A.plane[what] + (u64)(unit < 0 ? 0 : unit) * A.unit_bytes[what];
+        char* cell = base + (u64)slot * A.token_bytes + (u64)h * A.head_bytes + d0 * (kE4m3 ? 1 : 2);
+        float* scale_at = reinterpret_cast<float*>(base + A.scale_off) + ((u64)h << A.shift) + slot;
+        if constexpr (kWrite) {
+            u32x4 w = {0, 0, 0, 0};
+            if (in) w = *reinterpret_cast<const u32x4*>(row);
+            if constexpr (!kE4m3) {
+                if (in) *reinterpret_cast<u32x4*>(cell) = w;
+            } else {
+                float x[8], top = 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    x[2 * j] = T::lo(w[j]);
+                    x[2 * j + 1] = T::hi(w[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float a = fabsf(x[j]);
+                    top = a < INFINITY && a > top ? a : top;        // NaN is neither
+                }
+#pragma unroll
+                for (int m = kLanes / 2; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+                const float scale = fmaxf(top / 448.f, 0x1p-126f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float q = x[j] / scale;
+                    x[j] = q > 448.f ? 448.f : q < -448.f ? -448.f : q;     // NaN stays
+                }
+                int lo = 0, hi = 0;
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], lo, false);
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], hi, false);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], hi, true);
+                if (in) *reinterpret_cast<u32x2*>(cell) = u32x2{(unsigned)lo, (unsigned)hi};
+                if (d0 == 0) *scale_at = scale;
+            }
+        } else {
+            u32x4 w = {0, 0, 0, 0};
+            if (unit >= 0 && in) {
+                if constexpr (!kE4m3) {
+                    w = *reinterpret_cast<const u32x4*>(cell);
+                } else {
+                    const u32x2 c = *reinterpret_cast<const u32x2*>(cell);
+                    const float s = *scale_at;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[j], false);
+                        const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[j], true);
+                        w[2 * j] = T::pack(a[0] * s, a[1] * s);
+                        w[2 * j + 1] = T::pack(b[0] * s, b[1] * s);
+                    }
+                }
+            }
+            if (in) *reinterpret_cast<u32x4*>(row) = w;
+        }
+    }
+}
+
+template <class T, bool kE4m3, bool kWrite>
+void cache_launch(const CacheArgs& A, hipStream_t st) {
+    const dim3 grid((A.n_rows + A.rows_per_block - 1) / A.rows_per_block), block(kCacheThreads);
+    if (A.dim <= 64) hipLaunchKernelGGL((k_cache<T, kE4m3, kWrite, 8>), grid, block, 0, st, A);
+    else if (A.dim <= 128) hipLaunchKernelGGL((k_cache<T, kE4m3, kWrite, 16>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_cache<T, kE4m3, kWrite, 32>), grid, block, 0, st, A);
+}
+
+template <bool kWrite>
+ss_status cache_call(const ss_kv_cache* c, const ss_batch* b, const void* k, const void* v,
+                     uint32_t type, u64 row_stride, u64 head_stride, void* stream) {
+    ss_status s = cache_args(c, type);
+    if (s == SS_OK) s = batch_args(b, true, false);
+    if (s != SS_OK) return s;
+    if (b->n_rows == 0 || b->n_requests == 0) return SS_OK;
+    for (const auto& x : {std::make_pair("k", k), std::make_pair("v", v)}) {
+        s = rows_args(x.first, x.second, b->n_rows, c->n_heads, c->head_dim, row_stride, head_stride,
+                      !kWrite);
+        if (s != SS_OK) return s;
+    }
+    int dev = -1;
+    if ((s = current_device(&dev)) != SS_OK || (s = cache_memory(c, dev)) != SS_OK ||
+        (s = batch_memory(b, true, false, dev)) != SS_OK)
+        return s;
+    const u64 bytes = rows_bytes(b->n_rows, c->n_heads, c->head_dim, row_stride, head_stride);
+    if (!device_range_ok(k, bytes, dev)) return device_error("k", dev);
+    if (!device_range_ok(v, bytes, dev)) return device_error("v", dev);
+    CacheArgs A{};
+    A.tab = table_of(c->units, c->agent_off, c->n_agents, c->n_entries, c->capacity_units);
+    A.plane[0] = static_cast<char*>(c->k);
+    A.plane[1] = static_cast<char*>(c->v);
+    A.unit_bytes[0] = c->k_unit_bytes;
+    A.unit_bytes[1] = c->v_unit_bytes;
+    A.token_bytes = c->token_bytes;
+    A.head_bytes = c->head_bytes;
+    A.scale_off = c->scale_off;
+    A.rows[0] = static_cast<char*>(const_cast<void*>(k));
+    A.rows[1] = static_cast<char*>(const_cast<void*>(v));
+    A.row_stride = 2 * row_stride;
+    A.head_stride = 2 * head_stride;
+    A.row_off = b->row_off;
+    A.agents = b->agents;
+    A.lens = b->lens;
+    A.n_rows = b->n_rows;
+    A.n_requests = b->n_requests;
+    A.n_heads = c->n_heads;
+    A.dim = c->head_dim;
+    A.shift = (unsigned)__builtin_ctz(c->page_tokens);
+    // the search for the rows' requests costs a block as much for one row as for
+    // 16, so blocks take more rows once there are 1,024 blocks
+    A.rows_per_block = 1;
+    while (A.rows_per_block < 16 && b->n_rows / (2 * A.rows_per_block) >= 1024) A.rows_per_block *= 2;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const bool q = c->type == SS_E4M3;
+    if (type == SS_BF16) {
+        if (q) cache_launch<Bf16, true, kWrite>(A, st);
+        else cache_launch<Bf16, false, kWrite>(A, st);
+    } else {
+        if (q) cache_launch<F16, true, kWrite>(A, st);
+        else cache_launch<F16, false, kWrite>(A, st);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess)
+        return set_err(SS_ERR_HIP, "%s kernel: %s", kWrite ? "kv write" : "kv read",
+                       hipGetErrorString(e));
+    return SS_OK;
+}
+
+bool aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// a + b * c where every term is nonnegative, or UINT64_MAX beyond 2^62.
+u64 madd(u64 a, u64 b, u64 c) {
+    const __uint128_t x = (__uint128_t)b * c + a;
+    return x > ((__uint128_t)1 << 62) ? UINT64_MAX : (u64)x;
+}
+
+// Bytes of a page's codes or values, behind k + unit * k_unit_bytes.
+u64 page_bytes(const ss_kv_cache* c) {
+    const u64 row = (u64)c->head_dim * (c->type == SS_E4M3 ? 1 : 2);
+    return madd(madd(row, c->page_tokens - 1, c->token_bytes), c->n_heads - 1, c->head_bytes);
+}
+u64 unit_span(const ss_kv_cache* c) {
+    const u64 body = page_bytes(c);
+    if (c->type != SS_E4M3) return body;
+    return std::max(body, madd(c->scale_off, 4ull * c->n_heads, c->page_tokens));
+}
+
+}  // namespace
+
+ss_status device_error(const char* name, int dev) {
+    return set_err(SS_ERR_ARG, "%s must be device memory of the current device (%d), large enough",
+                   name, dev);
+}
+
+ss_status table_args(const int32_t* units, const uint64_t* agent_off, uint32_t n_agents,
+                     uint64_t n_entries, uint64_t capacity_units) {
+    if (!units || !agent_off) return set_err(SS_ERR_ARG, "NULL block table");
+    if (n_agents < 1 || n_entries < 1 || n_entries >= (1ull << 40))
+        return set_err(SS_ERR_ARG, "n_agents and n_entries must be >= 1");
+    if (capacity_units < 1 || capacity_units >= (1ull << 31))
+        return set_err(SS_ERR_ARG, "capacity_units must be in [1, 2^31)");
+    return SS_OK;
+}
+
+ss_status cache_args(const ss_kv_cache* c, uint32_t row_type) {
+    if (!c) return set_err(SS_ERR_ARG, "cache is NULL");
+    ss_status s = table_args(c->units, c->agent_off, c->n_agents, c->n_entries, c->capacity_units);
+    if (s != SS_OK) return s;
+    if (!c->k || !c->v || !aligned(c->k) || !aligned(c->v))
+        return set_err(SS_ERR_ARG, "cache k and v must be 16-byte aligned pointers");
+    if (c->page_tokens < 1 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1)))
+        return set_err(SS_ERR_ARG, "page_tokens must be a power of two in [1, 1024]");
+    if (c->n_heads < 1 || c->n_heads > 1024)
+        return set_err(SS_ERR_ARG, "n_heads must be in [1, 1024]");
+    if (c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16)
+        return set_err(SS_ERR_ARG, "head_dim must be a multiple of 16 in [16, 256]");
+    if (c->type != SS_BF16 && c->type != SS_F16 && c->type != SS_E4M3)
+        return set_err(SS_ERR_ARG, "unknown cache type %u", c->type);
+    if (row_type != SS_BF16 && row_type != SS_F16)
+        return set_err(SS_ERR_ARG, "rows must be SS_BF16 or SS_F16, not type %u", row_type);
+    if (c->type != SS_E4M3 && c->type != row_type)
+        return set_err(SS_ERR_ARG, "rows of type %u with a cache of type %u", row_type, c->type);
+    for (u64 x : {c->k_unit_bytes, c->v_unit_bytes, c->token_bytes, c->head_bytes, c->scale_off})
+        if (x % 16) return set_err(SS_ERR_ARG, "cache byte distances must be multiples of 16");
+    // tokens within heads or heads within tokens, rows apart from each other
+    const u64 row = (u64)c->head_dim * (c->type == SS_E4M3 ? 1 : 2);
+    const bool by_head = (c->page_tokens == 1 || c->token_bytes >= row) &&
+        (c->n_heads == 1 || c->head_bytes >= madd(row, c->page_tokens - 1, c->token_bytes));
+    const bool by_token = (c->n_heads == 1 || c->head_bytes >= row) &&
+        (c->page_tokens == 1 || c->token_bytes >= madd(row, c->n_heads - 1, c->head_bytes));
+    if (!by_head && !by_token) return set_err(SS_ERR_ARG, "a page's rows overlap");
+    if (c->type == SS_E4M3 && c->scale_off < page_bytes(c))
+        return set_err(SS_ERR_ARG, "scale_off lies inside the page's codes");
+    const u64 span = unit_span(c);
+    if (c->capacity_units > 1 && (c->k_unit_bytes < span || c->v_unit_bytes < span))
+        return set_err(SS_ERR_ARG, "a page of %llu bytes does not fit into a unit's chunk",
+                       (unsigned long long)span);
+    if (madd(span, c->capacity_units - 1, std::max(c->k_unit_bytes, c->v_unit_bytes)) == UINT64_MAX)
+        return set_err(SS_ERR_ARG, "cache sizes are too large");
+    return SS_OK;
+}
+
+ss_status batch_args(const ss_batch* b, bool lens, bool groups) {
+    if (!b) return set_err(SS_ERR_ARG, "batch is NULL");
+    if (b->n_rows >= (1u << 31)) return set_err(SS_ERR_ARG, "n_rows must be below 2^31");
+    if (b->n_requests >= (1u << 20)) return set_err(SS_ERR_ARG, "n_requests must be below 2^20");
+    if (groups && b->n_groups >= (1u << 20))
+        return set_err(SS_ERR_ARG, "n_groups must be below 2^20");
+    if (b->n_rows == 0 || b->n_requests == 0) return SS_OK;
+    if (!b->row_off || !b->agents || (lens && !b->lens))
+        return set_err(SS_ERR_ARG, "NULL array in the batch");
+    if (groups && b->n_groups && (!b->group_off || !b->prefix_agents || !b->prefix_lens))
+        return set_err(SS_ERR_ARG, "NULL array of the batch's groups");
+    return SS_OK;
+}
+
+ss_status rows_args(const char* name, const void* ptr, u64 n_rows, u64 n_heads, u64 dim,
+                    u64 row_stride, u64 head_stride, bool written) {
+    if (!ptr || !aligned(ptr)) return set_err(SS_ERR_ARG, "%s must be a 16-byte aligned pointer", name);
+    if (row_stride % 8 || head_stride % 8)
+        return set_err(SS_ERR_ARG, "strides of %s must be multiples of 8 elements", name);
+    if (row_stride >= (1ull << 40) || head_stride >= (1ull << 40))
+        return set_err(SS_ERR_ARG, "strides of %s are too large", name);
+    // written rows do not overlap: heads within rows or rows within heads
+    if (written && !((n_heads == 1 || head_stride >= dim) &&
+                     (n_rows == 1 || row_stride >= madd(dim, n_heads - 1, head_stride))) &&
+        !((n_rows == 1 || row_stride >= dim) &&
+          (n_heads == 1 || head_stride >= madd(dim, n_rows - 1, row_stride))))
+        return set_err(SS_ERR_ARG, "rows of %s overlap", name);
+    if (rows_bytes(n_rows, n_heads, dim, row_stride, head_stride) >= (1ull << 62))
+        return set_err(SS_ERR_ARG, "%s is too large", name);
+    return SS_OK;
+}
+
+u64 rows_bytes(u64 n_rows, u64 n_heads, u64 dim, u64 row_stride, u64 head_stride) {
+    const u64 n = madd(madd(dim, n_rows - 1, row_stride), n_heads - 1, head_stride);
+    return n > (1ull << 61) ? UINT64_MAX : 2 * n;
+}
+
+ss_status current_device(int* dev) {
+    if (hipGetDevice(dev) != hipSuccess) {
+        (void)hipGetLastError();
+        return set_err(SS_ERR_ARG, "no current device");
+    }
+    return SS_OK;
+}
+
+ss_status table_memory(const int32_t* units, const uint64_t* agent_off, uint32_t n_agents,
+                       uint64_t n_entries, int dev) {
+    if (!device_range_ok(units, n_entries * 4, dev)) return device_error("units", dev);
+    if (!device_range_ok(agent_off, ((u64)n_agents + 1) * 8, dev))
+        return device_error("agent_off", dev);
+    return SS_OK;
+}
+
+ss_status cache_memory(const ss_kv_cache* c, int dev) {
+    const ss_status s = table_memory(c->units, c->agent_off, c->n_agents, c->n_entries, dev);
+    if (s != SS_OK) return s;
+    const u64 span = unit_span(c);
+    if (!device_range_ok(c->k, madd(span, c->capacity_units - 1, c->k_unit_bytes), dev))
+        return device_error("cache k", dev);
+    if (!device_range_ok(c->v, madd(span, c->capacity_units - 1, c->v_unit_bytes), dev))
+        return device_error("cache v", dev);
+    return SS_OK;
+}
+
+ss_status batch_memory(const ss_batch* b, bool lens, bool groups, int dev) {
+    if (!device_range_ok(b->row_off, ((u64)b->n_requests + 1) * 4, dev))
+        return device_error("row_off", dev);
+    if (!device_range_ok(b->agents, (u64)b->n_requests * 4, dev)) return device_error("agents", dev);
+    if (lens && !device_range_ok(b->lens, (u64)b->n_requests * 4, dev))
+        return device_error("lens", dev);
+    if (!groups || b->n_groups == 0) return SS_OK;
+    if (!device_range_ok(b->group_off, ((u64)b->n_groups + 1) * 4, dev))
+        return device_error("group_off", dev);
+    if (!device_range_ok(b->prefix_agents, (u64)b->n_groups * 4, dev))
+        return device_error("prefix_agents", dev);
+    if (!device_range_ok(b->prefix_lens, (u64)b->n_groups * 4, dev))
+        return device_error("prefix_lens", dev);
+    return SS_OK;
+}
+
+}  // namespace ss
+
+using namespace ss;
+
+extern "C" {
+
+ss_status ss_kv_write(const ss_kv_cache* cache, const ss_batch* batch, const void* k,
+                      const void* v, uint32_t type, uint64_t row_stride, uint64_t head_stride,
+                      void* stream) {
+    return cache_call<true>(cache, batch, k, v, type, row_stride, head_stride, stream);
+}
+
+ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, void* v,
+                     uint32_t type, uint64_t row_stride, uint64_t head_stride, void* stream) {
+    return cache_call<false>(cache, batch, k, v, type, row_stride, head_stride, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,278 @@
+"""ss_prefix_attention against the plain form in 64 bits: lengths from none to
+long, page sizes, head layouts and widths, shared prefixes of many and few
+requests, agents that are away, NaN where no token is, and rows of nobody.
+
+The bound of an output, per element (u16: half a step of the stored weight's
+type, out: of the output's): scores are sums of exact products in 32 bits, so each
+is off by at most e = (dim + 4) 2^-24 scale sum|q k| + 2^-21 (the exponent's own
+rounding at |score| <= 8, more below through e), weights by a factor e^e and, when
+rounded, u16 (fp16 weights below 2^-14 by 2^-25 of the largest weight); sums of n
+terms in 32 bits add n 2^-24.  That makes
+    (u16 + 4 e + (n + 64) 2^-24) sum w |v| + n 2^-25 max|v| [fp16] + out |o|.
+log-sums are off by 2 e + (n + 64) 2^-24 + 2^-22 |lse|."""
+import numpy as np
+import pytest
+
+from model_harness import SENTINEL, Batch, Cache, Rows, up
+from oracle import model as M
+from paper_2601_21473_amd import binding as B
+from paper_2601_21473_amd.memory import DeviceBuffer
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert B.device_count() > 0, "GPU tests need a GPU"
+
+
+def expected(cache, batch, q, per, scale):
+    """Per row of the batch: out, lse, sum w|v|, max|v|, max scale sum|qk|, keys."""
+    n, h, d = int(batch.row_off[-1]), cache.heads, cache.dim
+    out = [np.zeros((n, h, per, d)), np.full((n, h, per), -np.inf), np.zeros((n, h, per, d)),
+           np.zeros((n, h, per, d)), np.zeros((n, h, per))]
+    count = np.zeros(n)
+    prefixes = {}
+    for r in range(len(batch.rows)):
+        rows = int(batch.rows[r])
+        if not rows:
+            continue
+        length = int(batch.lens[r])
+        at = slice(int(batch.row_off[r]), int(batch.row_off[r]) + rows)
+        a = int(batch.agents[r])
+        pages = int(cache.off[a + 1] - cache.off[a]) if a < len(cache.lens) else 0
+        have = min(length, pages * cache.page)
+        k, v, there = cache.tokens(a, have)
+        seen = (np.arange(have) <= (length - rows + np.arange(rows))[:, None]) & there
+        p = batch.prefix_of(r)
+        if p is not None:
+            if p not in prefixes:
+                pages = int(cache.off[p[0] + 1] - cache.off[p[0]]) if p[0] < len(cache.lens) else 0
+                prefixes[p] = cache.tokens(p[0], min(p[1], pages * cache.page))
+            pk, pv, pt = prefixes[p]
+            k, v = np.concatenate([pk, k]), np.concatenate([pv, v])
+            seen = np.concatenate([np.broadcast_to(pt, (rows, len(pt))), seen], 1)
+        got = M.attention(q[at].reshape(rows, h, per, d), k, v, seen, scale)
+        for o, x in zip(out, got):
+            o[at] = x
+        count[at] = len(k)
+    return out, count
+
+
+def attend(cache, batch, q, per, kind, *, scale, lse=True, out_layout=None, stream=0):
+    heads = cache.heads * per
+    out = Rows(batch.n_rows, heads, cache.dim, kind, **(out_layout or {}))
+    d_lse = up(np.full(batch.n_rows * heads, 12345.0, np.float32))
+    need = B.prefix_attention_workspace(cache.desc, batch.desc, heads)
+    assert need > 0
+    ws = DeviceBuffer(need)
+    B.prefix_attention(cache.desc, batch.desc, q.ptr, out.ptr, type=kind, n_q_heads=heads,
+                       q_strides=q.strides, out_strides=out.strides, scale=scale, workspace=ws.ptr,
+                       workspace_bytes=need, lse=d_lse.ptr if lse else 0, stream=stream)
+    B.stream_sync(stream)
+    got, clean = out.bits()
+    assert clean, "bytes outside the rows were written"
+    l = d_lse.download(0, 4 * batch.n_rows * heads).view(np.float32).reshape(batch.n_rows, heads)
+    for x in (ws, out, d_lse):
+        x.free()
+    return got, l
+
+
+def check(cache, batch, q, per, kind, got, lse, scale):
+    (o, l, mag, big, size), count = expected(cache, batch, q.before()[:int(batch.row_off[-1])], per, scale)
+    n = len(count)
+    o, mag, big = (x.reshape(n, -1, cache.dim) for x in (o, mag, big))
+    l, size = l.reshape(n, -1), size.reshape(n, -1)
+    e = (cache.dim + 4) * 2.0 ** -24 * size + 2.0 ** -21
+    terms = (count[:, None] + 64) * 2.0 ** -24
+    stored = M.BF16 if cache.kind == M.E4M3 else kind
+    value = M.from_bits(got[:n], kind)
+    tol = (M.HALF_STEP[stored] + 4 * e + terms)[..., None] * mag + M.HALF_STEP[kind] * np.abs(o)
+    if stored == M.F16:
+        tol = tol + count[:, None, None] * 2.0 ** -25 * big
+    if kind == M.F16:
+        tol = tol + 2.0 ** -25                       # outputs below 2^-14
+    # a row that sees a NaN (a token that nobody wrote) is NaN, and no other row
+    nan = np.isnan(o)
+    assert np.array_equal(np.isnan(value), nan) and np.array_equal(np.isnan(lse[:n]), np.isnan(l))
+    worst = np.where(nan, 0, np.abs(value - o) - tol)
+    assert (worst <= 0).all(), (np.argwhere(worst > 0)[:4], np.nanmax(np.abs(value - o)), np.nanmin(tol))
+    nothing = np.isneginf(l)
+    assert (np.isneginf(lse[:n]) == nothing).all()
+    assert (got[:n][nothing] == 0).all()
+    some = np.isfinite(l)
+    ltol = 2 * e + terms + 2.0 ** -22 * np.abs(np.where(some, l, 0))
+    assert (np.abs(lse[:n][some] - l[some]) <= ltol[some]).all()
+    assert (got[n:] == SENTINEL * 0x101).all() and (lse[n:] == 12345.0).all(), "rows of nobody"
+
+
+def run(cache, batch, per, kind, seed=0, pad=0, by_head=False, scale=None, size=1.0):
+    rng = np.random.default_rng(seed)
+    scale = 1 / np.sqrt(cache.dim) if scale is None else scale
+    scale = float(np.float32(scale))
+    q = Rows(batch.n_rows, cache.heads * per, cache.dim, kind, pad=pad, by_head=by_head,
+             values=size * rng.standard_normal((batch.n_rows, cache.heads * per, cache.dim)))
+    got, lse = attend(cache, batch, q, per, kind, scale=scale,
+                      out_layout=dict(pad=8 - pad if pad else 0, by_head=not by_head))
+    check(cache, batch, q, per, kind, got, lse, scale)
+    for x in (q, batch, cache):
+        x.free()
+    return got
+
+
+KINDS = [(M.BF16, M.BF16), (M.F16, M.F16), (M.E4M3, M.BF16), (M.E4M3, M.F16)]
+
+
+@pytest.mark.parametrize("kind,rows_kind", KINDS)
+@pytest.mark.parametrize("page,heads,per,dim,order,gap", [
+    (16, 2, 2, 64, "token", 0), (16, 1, 4, 128, "head", 0), (1, 2, 1, 16, "head", 16),
+    (4, 3, 3, 80, "token", 16), (64, 1, 7, 256, "head", 0), (32, 2, 20, 144, "token", 0),
+    (1024, 1, 1, 48, "head", 32), (8, 1, 16, 112, "token", 0), (16, 1, 17, 240, "head", 16)])
+def test_single_tokens(kind, rows_kind, page, heads, per, dim, order, gap):
+    """Decoding: lengths from 1 over every place of a 64-key block to a few
+    hundred, one row a request, spare rows behind."""
+    lens = [1, 2, 15, 16, 17, 31, 33, 63, 64, 65, 127, 129, 200, 257, 319]
+    rng = np.random.default_rng(dim)
+    cache = Cache(rng, lens, page=page, heads=heads, dim=dim, kind=kind, order=order, gap=gap)
+    batch = Batch([1] * len(lens), np.arange(len(lens)), lens, spare=3)
+    run(cache, batch, per, rows_kind, seed=page, pad=8 if gap else 0, by_head=order == "token")
+
+
+@pytest.mark.parametrize("kind,rows_kind", KINDS)
+@pytest.mark.parametrize("rows,lens,per", [
+    ([5, 1, 0, 17, 64], [5, 9, 3, 17, 64], 1), ([70, 3], [200, 3], 2), ([130, 2, 33], [130, 150, 40], 4),
+    ([1, 2, 3, 4, 5, 6, 7, 8, 9], [1, 2, 3, 4, 5, 60, 70, 80, 90], 8), ([200], [200], 5)])
+def test_prompts(kind, rows_kind, rows, lens, per):
+    """Several rows a request, each seeing up to its own token."""
+    rng = np.random.default_rng(sum(rows))
+    cache = Cache(rng, lens, page=16, heads=2, dim=128 if per < 5 else 64, kind=kind)
+    run(cache, Batch(rows, np.arange(len(rows)), lens, spare=1), per, rows_kind)
+
+
+@pytest.mark.parametrize("kind,rows_kind", KINDS)
+@pytest.mark.parametrize("prefix", [1, 16, 63, 64, 100, 700])
+@pytest.mark.parametrize("shape", ["decode", "few rows", "prompts", "one each"])
+def test_shared_prefixes(kind, rows_kind, prefix, shape):
+    """Groups over prefixes: many requests of one row, of a few, prompts, groups of one
+    request, requests without a prefix before and behind, an empty group."""
+    rng = np.random.default_rng(prefix)
+    rows = {"decode": [1] * 11, "few rows": [1, 3, 2, 5, 4, 1, 1, 2, 6, 1, 2],
+            "prompts": [40, 70, 33, 1, 90], "one each": [2, 1, 30]}[shape]
+    n = len(rows)
+    lens = [int(r + x) for r, x in zip(rows, rng.integers(0, 60, n))]
+    groups = {"decode": [0, 1, 7, 7, 10], "few rows": [1, 4, 9], "prompts": [0, 3, 5],
+              "one each": [0, 1, 2, 3]}[shape]
+    g = len(groups) - 1
+    plens = [max(1, prefix - 3 * i) for i in range(g)]
+    order = rng.permutation(n + g)
+    by_agent = np.zeros(n + g, np.int64)
+    by_agent[order] = lens + plens
+    cache = Cache(rng, by_agent, page=16, heads=2, dim=128, kind=kind,
+                  order="token" if prefix % 2 else "head")
+    batch = Batch(rows, order[:n], lens, (groups, order[n:].tolist(), plens), spare=2)
+    run(cache, batch, 3, rows_kind, seed=prefix)
+
+
+@pytest.mark.parametrize("kind,rows_kind", KINDS)
+@pytest.mark.parametrize("page,dim", [(2, 64), (16, 256), (16, 96)])
+def test_shared_prefix_of_odd_layouts(kind, rows_kind, page, dim):
+    rng = np.random.default_rng(dim)
+    lens, plen = [3, 70, 1, 18, 9, 33], 150
+    cache = Cache(rng, lens + [plen], page=page, heads=1, dim=dim, kind=kind, gap=16)
+    run(cache, Batch([1, 2, 1, 1, 3, 1], range(6), lens, ([0, 6], [6], [plen])), 6, rows_kind, pad=8)
+
+
+@pytest.mark.parametrize("kind,rows_kind", [(M.BF16, M.BF16), (M.E4M3, M.F16)])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_large_tiles(kind, rows_kind, rows):
+    """Stacks of more rows than the largest tile over a prefix of many blocks."""
+    rng = np.random.default_rng(rows)
+    n = 90 if rows == 1 else 4
+    lens = [int(rows + x) for x in rng.integers(0, 90, n)]
+    cache = Cache(rng, lens + [1500], page=16, heads=1, dim=128, kind=kind)
+    run(cache, Batch([rows] * n, range(n), lens, ([0, n], [n], [1500])), 4, rows_kind)
+
+
+@pytest.mark.parametrize("kind,rows_kind", KINDS)
+def test_away_and_out_of_range(kind, rows_kind):
+    """Agents and prefixes that are away, agents that do not exist, lengths behind
+    the pages, lengths below the rows, and rows that see nothing at all."""
+    rng = np.random.default_rng(3)
+    lens = [40, 50, 0, 33, 20, 0, 64]
+    cache = Cache(rng, lens + [100, 80], page=16, heads=2, dim=64, kind=kind, away=(1, 8))
+    # the last page of agent 3 alone is away
+    first, last = int(cache.off[3]), int(cache.off[4])
+    cache.units[last - 1] = -1
+    cache.units[first] = cache.capacity + 5          # not a unit
+    cache.d_units.upload(cache.units)
+    cache.units[first] = -1
+    batch = Batch([1, 2, 1, 4, 1, 1, 1, 2, 5, 3], [0, 1, 2, 3, 4, 5, 9, 0xFFFFFFFF, 0, 6],
+                  [40, 50, 0, 33, 60, 3, 5, 2, 3, 64],
+                  ([0, 2, 4, 6, 8], [7, 8, 99, 8], [100, 80, 50, 70]))
+    got = run(cache, batch, 2, rows_kind)
+    assert got.any()
+
+
+def test_nothing_at_all():
+    """Every request away, with a group: zeros and -infinity come out all the same."""
+    rng = np.random.default_rng(4)
+    cache = Cache(rng, [10, 20, 30], page=16, heads=1, dim=64, kind=M.BF16, away=(0, 1, 2))
+    run(cache, Batch([1, 1, 2], [0, 1, 1], [10, 20, 20], ([0, 2], [2], [30])), 2, M.BF16)
+
+
+@pytest.mark.parametrize("kind,rows_kind", [(M.BF16, M.BF16), (M.E4M3, M.BF16), (M.F16, M.F16)])
+def test_long(kind, rows_kind):
+    """Few rows over many tokens: split over many workgroups and joined, with the
+    largest score far from the first block."""
+    rng = np.random.default_rng(5)
+    cache = Cache(rng, [9000, 4000, 70], page=16, heads=1, dim=64, kind=kind, order="token", spread=2.0)
+    run(cache, Batch([1, 2, 1], [0, 1, 2], [9000, 4000, 70]), 2, rows_kind, size=1.5)
+    cache = Cache(rng, [9000, 40, 70], page=16, heads=1, dim=128, kind=kind)
+    run(cache, Batch([1, 2], [1, 2], [40, 70], ([0, 2], [0], [9000])), 2, rows_kind)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0])
+def test_scales(scale):
+    rng = np.random.default_rng(6)
+    cache = Cache(rng, [100, 3], page=16, heads=1, dim=64, kind=M.BF16, spread=0.5)
+    run(cache, Batch([1, 3], [0, 1], [100, 3]), 2, M.BF16, scale=scale, size=0.5)
+
+
+def test_many_requests():
+    """More requests than one pass of the planning workgroup takes."""
+    rng = np.random.default_rng(10)
+    n = 2500
+    lens = rng.integers(1, 40, n)
+    cache = Cache(rng, lens, page=16, heads=1, dim=16, kind=M.BF16)
+    rows = np.minimum(lens, rng.integers(0, 3, n))
+    run(cache, Batch(rows, range(n), lens, ([0, 5, 1200, 2400], [0, 1, 2], [int(x) for x in lens[:3]])),
+        1, M.BF16)
+
+
+def test_same_result_every_time_and_without_lse():
+    rng = np.random.default_rng(11)
+    lens = [300, 20, 77, 150]
+    cache = Cache(rng, lens + [900], page=16, heads=2, dim=128, kind=M.BF16)
+    batch = Batch([1, 2, 1, 1], range(4), lens, ([0, 4], [4], [900]))
+    q = Rows(batch.n_rows, 8, 128, M.BF16, values=rng.standard_normal((batch.n_rows, 8, 128)))
+    first, lse = attend(cache, batch, q, 4, M.BF16, scale=0.1)
+    s = B.Stream()
+    for stream in (0, s.handle, 0):
+        again, lse2 = attend(cache, batch, q, 4, M.BF16, scale=0.1, stream=stream)
+        assert np.array_equal(first, again) and np.array_equal(lse, lse2)
+    again, lse2 = attend(cache, batch, q, 4, M.BF16, scale=0.1, lse=False)
+    assert np.array_equal(first, again) and (lse2 == 12345.0).all()
+    s.close()
+
+
+def test_offsets_that_break_the_rules_end():
+    """Decreasing and too large offsets: unspecified results, but the call ends and
+    writes nothing outside its rows."""
+    rng = np.random.default_rng(12)
+    cache = Cache(rng, [30, 40, 50], page=16, heads=1, dim=64, kind=M.BF16)
+    for off in ([0, 4, 2, 6], [0, 100, 3, 6], [5, 6, 0, 6], [0, 6, 0, 6]):
+        batch = Batch([2, 2, 2], [0, 1, 2], [30, 40, 50], ([0, 3], [2], [50]), spare=2)
+        batch.bufs[0].upload(np.array(off, np.uint32))
+        q = Rows(batch.n_rows, 2, 64, M.BF16, values=np.ones((batch.n_rows, 2, 64)))
+        attend(cache, batch, q, 2, M.BF16, scale=0.1)
+        batch.free()
