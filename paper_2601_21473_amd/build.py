@@ -5,6 +5,8 @@
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -32,13 +34,21 @@ SANITIZE_FLAGS = ["-O1", "-g", "-Xarch_host", "-fsanitize=address", "-Xarch_host
 
 def build(verbose: bool = False, out: str = LIB, sanitize: bool = False) -> str:
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
+    flags = [*FLAGS, *(SANITIZE_FLAGS if sanitize else [])]
     tmp = out + ".tmp"
-    cmd = [HIPCC, *FLAGS, *(SANITIZE_FLAGS if sanitize else []), *srcs, "-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + r.stdout + r.stderr)
+
+    def hipcc(*args):
+        cmd = [HIPCC, *flags, *args]
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + r.stdout + r.stderr)
+
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(len(srcs)) as pool:
+        objects = [os.path.join(d, s + ".o") for s in SOURCES]
+        list(pool.map(lambda so: hipcc("-c", so[0], "-o", so[1]), zip(srcs, objects)))
+        hipcc(*objects, "-o", tmp)
     os.replace(tmp, out)
     return out
 

@@ -11,6 +11,7 @@
 //     m = max_i m_i,  l = sum_i l_i 2^(m_i - m),  out = sum_i o_i 2^(m_i - m) / l.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ss_model.h"
 
@@ -22,7 +23,7 @@ constexpr unsigned kNone = 0xffffffffu;
 constexpr unsigned kBlock = 64;             // keys of one step of an item
 constexpr unsigned kTarget = 1024;          // items that a call is split into at least, if it can
 constexpr unsigned kMinBlocks = 4;          // and key blocks that an item has at least
-constexpr unsigned kTileRows = 16;
+constexpr unsigned kMostRows = 128;         // rows of the largest tile
 
 struct Stack {
     u64 first[2];       // table entries of the two segments of keys: prefix, own tokens
@@ -54,9 +55,11 @@ struct AttendArgs {
     unsigned n_rows, n_requests, n_groups;
     unsigned n_heads, per;                      // key/value heads, query heads of each
     unsigned dim, shift;
-    float scale;                                // times log2(e)
+    float scale;                                // |scale| log2(e), 1 for a scale of 0
+    unsigned q_keep, q_flip;                    // queries' bits that count, and that turn
     // workspace
-    unsigned* n_items;                          // items per head; 1 where the offsets are valid
+    unsigned* n_items;                          // items per head; 1 where the offsets are valid;
+                                                // items taken
     unsigned* item0;                            // [stacks + 1] first item of each stack
     Stack* stacks;                              // [n_requests + n_groups]
     float* part_o;                              // [part_rows][padded dim]
@@ -101,8 +104,15 @@ __device__ bool pooled(const AttendArgs& A, unsigned g, unsigned* row0, unsigned
 __device__ unsigned blocks_of(const Stack& s) {
     return (s.keys[0] + kBlock - 1) / kBlock + (s.keys[1] + kBlock - 1) / kBlock;
 }
+// Rows of a stack's tiles: 16 while they hold all (nothing to share, so registers
+// suffice), else 64 or 128 through LDS.
+__device__ unsigned tile_rows(const AttendArgs& A, const Stack& s) {
+    const u64 rows = (u64)s.rows * A.per;
+    return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+}
 __device__ u64 tiles_of(const AttendArgs& A, const Stack& s) {
-    return ((u64)s.rows * A.per + kTileRows - 1) / kTileRows;
+    const unsigned n = tile_rows(A, s);
+    return ((u64)s.rows * A.per + n - 1) / n;
 }
 
 __device__ Stack stack_of(const AttendArgs& A, unsigned s) {
@@ -117,12 +127,15 @@ __device__ Stack stack_of(const AttendArgs& A, unsigned s) {
         const long long see = (long long)len - t.rows;
         t.see = (int)(see < -1 - (long long)t.rows ? -1 - (long long)t.rows
                                                    : see > 0x7fffffff ? 0x7fffffff : see);
-        t.keys[1] = tokens_with_page(A, A.agents[s], len, &t.first[1]);
+        u64 first;
+        t.keys[1] = tokens_with_page(A, A.agents[s], len, &first);
+        t.first[1] = first;
         const unsigned g = A.n_groups ? group_of(A, s) : kNone;
         if (g != kNone) {
             unsigned row0, rows;
             if (pooled(A, g, &row0, &rows)) t.pool = A.n_requests + g;
-            else t.keys[0] = tokens_with_page(A, A.prefix_agents[g], A.prefix_lens[g], &t.first[0]);
+            else t.keys[0] = tokens_with_page(A, A.prefix_agents[g], A.prefix_lens[g], &first);
+            if (t.keys[0]) t.first[0] = first;
         }
     } else {
         const unsigned g = s - A.n_requests;
@@ -130,7 +143,9 @@ __device__ Stack stack_of(const AttendArgs& A, unsigned s) {
         if (!pooled(A, g, &row0, &rows)) return t;
         t.row0 = row0;
         t.rows = rows;
-        t.keys[0] = tokens_with_page(A, A.prefix_agents[g], A.prefix_lens[g], &t.first[0]);
+        u64 first;
+        t.keys[0] = tokens_with_page(A, A.prefix_agents[g], A.prefix_lens[g], &first);
+        t.first[0] = first;
     }
     return t;
 }
@@ -225,228 +240,371 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
         A.item0[n] = fits ? (unsigned)s_base[0] : 0;
         A.n_items[0] = fits ? (unsigned)s_base[0] : 0;
         A.n_items[1] = fits && valid;
+        A.n_items[2] = 0;
     }
 }
 
 constexpr int kWaves = 4;
+// A weight may pass the running reference by 2^kSlack before sums are rescaled:
+// the reference then stays for most blocks, and a block's maximum need not be known
+// to all lanes of a row.  2^8 is exact in every type and far from their ranges.
+constexpr float kSlack = 8.f;
 
-// The output (or partial) of `rows` rows of an item whose sums the workgroup
-// holds in LDS: o[row][kDim + 4], ml[row] = maximum, sum.
-struct Sink {
-    const AttendArgs& A;
-    const Stack& s;
-    unsigned tile_row;          // first stack row of the item
-    unsigned split, head;
-    __device__ u64 part_row(unsigned m) const {
-        const u64 total = (u64)s.rows * A.per;
-        return s.part + ((u64)head * s.splits + split) * total + m;
+// A lane's share of 16 keys and values as they come from memory, and where it lies.
+// Products want S^T = K Q^T and O^T = V^T P^T with 16 x 16 x 32 products:
+//   K: a lane holds key lane % 16, dims 8 q .. 8 q + 7 of each 32 (q = lane / 16); for
+//      e4m3 it loads 16 codes at once, so its dims are 16 q .. + 15 of each 64, which
+//      the queries follow (slot_dim);
+//   S^T leaves it with the scores of row lane % 16 for keys 4 q .. 4 q + 3;
+//   V: it loads dim / 16 columns of those four keys, so a quarter wave reads whole
+//      rows, and pairs keys up by byte permutes: product i yields the columns
+//      lane * (dim / 16) + i.  Key slot 8 q + j of 32 is key 16 (j / 4) + 4 q + j % 4,
+//      which is how the weights lie in S^T: they never leave their lane.
+template <class T, int kDim, bool kE4m3>
+struct Keys {
+    static constexpr int kCols = kDim / 16, kFrags = kDim / 32;
+    static constexpr int kLoads = kE4m3 ? kFrags / 2 : kFrags;
+    static constexpr int kWords = kE4m3 ? kCols / 4 : kCols / 2;
+    typedef typename std::conditional<kE4m3, Bf16, T>::type P;  // weights times scales need range
+    typedef unsigned wide __attribute__((ext_vector_type(kWords == 1 ? 2 : kWords)));
+    u32x4 k[kLoads];
+    unsigned v[4][kWords];
+    f32x4 ks, vs;
+
+    static __device__ unsigned slot_dim(unsigned f, unsigned quad) {
+        return kE4m3 ? 64 * (f / 2) + 16 * quad + 8 * (f % 2) : 32 * f + 8 * quad;
+    }
+    // Fragment f of the keys.
+    __device__ u32x4 key(int f) const {
+        if constexpr (kE4m3) {
+            const unsigned a = k[f / 2][2 * (f % 2)], b = k[f / 2][2 * (f % 2) + 1];
+            return u32x4{T::template from_e4m3<false>(a), T::template from_e4m3<true>(a),
+                         T::template from_e4m3<false>(b), T::template from_e4m3<true>(b)};
+        } else {
+            return k[f];
+        }
+    }
+    // Words w (columns 2 w, 2 w + 1) of value i in 16 bits.
+    __device__ unsigned value(int i, int w) const {
+        if constexpr (kE4m3)
+            return w % 2 ? P::template from_e4m3<true>(v[i][w / 2]) : P::template from_e4m3<false>(v[i][w / 2]);
+        else
+            return v[i][w];
     }
 };
 
-// 16 rows and a range of keys.  The four waves take 64-key blocks in turn, each
-// with a running maximum and sum of its own, and join at the end: with so few
-// rows a key or value is used once, so it goes from memory to registers and
-// through the matrix product without a stop in LDS.
-//     S^T = K Q^T:  a lane holds the scores of one row (lane % 16) with four keys
-//                   of each 16 (quad q = lane / 16: keys 4 q .. 4 q + 3);
-//     O^T = V^T P^T: P^T is read in just that layout (key slot 8 q + j of 32 keys is
-//                   key 16 (j / 4) + 4 q + j % 4), so weights never leave their lane.
-// V^T wants eight keys of one column in a lane: a lane loads kCols = dim / 16
-// columns of its eight keys, whole rows per quarter wave, and pairs them up by
-// byte permutes (column lane * kCols + i in product i).
+// The lane's constant part of the addresses.
 template <class T, int kDim, bool kE4m3>
-__device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, unsigned tile,
-                         unsigned split, float* lds_o, float2* lds_ml) {
-    typedef typename std::conditional<kE4m3, Bf16, T>::type P;      // weights times scales: range
-    constexpr int kCols = kDim / 16, kFrags = kDim / 32;
-    constexpr int kSub = kDim > 128 ? 2 : 4;        // 16-key sub-blocks held at a time
-    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const unsigned col = lane % 16, quad = lane / 16;
-    const unsigned total = s.rows * A.per;
-    const unsigned m = tile * kTileRows + col;              // this lane's stack row
-    const unsigned row = m / A.per, g = m - row * A.per;
-    // own tokens that this lane's row sees
-    const int lim = m < total ? (int)min((long long)s.keys[1], max(0ll, (long long)s.see + row + 1)) : 0;
-    const unsigned last = min(total - 1, tile * kTileRows + kTileRows - 1) / A.per;
-    const unsigned most = (unsigned)min((long long)s.keys[1], max(0ll, (long long)s.see + last + 1));
-    const unsigned nb0 = (s.keys[0] + kBlock - 1) / kBlock;
-    const unsigned nb = nb0 + (most + kBlock - 1) / kBlock;
-    const u64 b0 = (u64)split * s.chunk;
-    const u64 b1 = min((u64)nb, b0 + s.chunk);
-
-    // Q: fragment f of 32 dims; slot 8 quad + j is dim 32 f + 8 quad + j, and for
-    // e4m3 (16 codes a load) dim 64 (f / 2) + 16 quad + 8 (f % 2) + j
-    u32x4 qf[kFrags];
-    unsigned kdim[kFrags];
+struct Places {
+    typedef Keys<T, kDim, kE4m3> K;
+    unsigned col, quad;
+    unsigned kd[K::kLoads], vd;     // byte offsets inside a row, 0 behind dim
+    __device__ Places(const AttendArgs& A) {
+        const unsigned lane = threadIdx.x % 64;
+        col = lane % 16;
+        quad = lane / 16;
 #pragma unroll
-    for (int f = 0; f < kFrags; ++f) {
-        kdim[f] = kE4m3 ? 64 * (f / 2) + 16 * quad + 8 * (f % 2) : 32 * f + 8 * quad;
-        qf[f] = u32x4{0, 0, 0, 0};
-        if (m < total && kdim[f] < A.dim)
-            qf[f] = *reinterpret_cast<const u32x4*>(A.q + (u64)(s.row0 + row) * A.q_row +
-                                                    (u64)(head * A.per + g) * A.q_head + 2 * kdim[f]);
+        for (int f = 0; f < K::kLoads; ++f) {
+            const unsigned d = K::slot_dim(kE4m3 ? 2 * f : f, quad);
+            kd[f] = d < A.dim ? d * (kE4m3 ? 1 : 2) : 0;
+        }
+        vd = col * K::kCols < A.dim ? col * K::kCols * (kE4m3 ? 1 : 2) : 0;
     }
-    f32x4 o[kCols];
-#pragma unroll
-    for (int i = 0; i < kCols; ++i) o[i] = f32x4{0, 0, 0, 0};
-    float top = -INFINITY, sum = 0.f;
-    const unsigned vdim = col * kCols < A.dim ? col * kCols : 0;    // columns behind dim: unused
-    const unsigned page_mask = (1u << A.shift) - 1u;
-    const char* kbase = A.k + (u64)head * A.head_bytes;
-    const char* vbase = A.v + (u64)head * A.head_bytes;
+};
 
-    for (u64 b = b0 + wave; b < b1; b += kWaves) {
-        const bool own = b >= nb0;
-        const unsigned key0 = (unsigned)(own ? b - nb0 : b) * kBlock;
-        const u64 first = s.first[own];
-        const unsigned limit = own ? most : s.keys[0];
-        // lane l looks up key l of the block
-        const unsigned key = key0 + lane;
-        int unit = -1;
-        if (key < limit) unit = A.tab.unit(first + (key >> A.shift));
-        const u64 there = __ballot(unit >= 0);
-        if (!there) continue;
-        const int spare = __shfl(unit, __builtin_ctzll(there));      // some unit that can be read
-        const int safe = unit >= 0 ? unit : spare;
+// Loads the 16 keys and values from key `key0` (a multiple of 16) on, whose units
+// lie in lanes `at` .. at + 15 of `unit`; tokens that are away are read from unit 0.
+// kWide: pages of 16 tokens and more, so the 16 keys are of one unit and their
+// address is the same for all lanes but for a 32-bit offset.
+template <class T, int kDim, bool kE4m3, bool kWide>
+__device__ __forceinline__ void load_keys(const AttendArgs& A, const Places<T, kDim, kE4m3>& p,
+                                          unsigned head, int unit, unsigned at, unsigned key0,
+                                          Keys<T, kDim, kE4m3>& x) {
+    typedef Keys<T, kDim, kE4m3> K;
+    const unsigned mask = (1u << A.shift) - 1u;
+    const u64 head_off = (u64)head * A.head_bytes;
+    auto k_from = [&](const char* row) {
 #pragma unroll
-        for (int s0 = 0; s0 < 4; s0 += kSub) {
-            float sc[kSub][4], kscale[kSub][4], vscale[kSub][4];
-            u64 vo[kSub][4];
-            f32x4 st[kSub];
-            u32x4 kf[kSub][kFrags];
-            unsigned vr[kSub][4][kCols / 2];
+        for (int f = 0; f < K::kLoads; ++f) x.k[f] = *reinterpret_cast<const u32x4*>(row + p.kd[f]);
+    };
+    auto v_from = [&](const char* row, int i) {
+        if constexpr (K::kWords == 1) {
+            x.v[i][0] = *reinterpret_cast<const unsigned*>(row);
+        } else {
+            const typename K::wide w = *reinterpret_cast<const typename K::wide*>(row);
 #pragma unroll
-            for (int t = 0; t < kSub; ++t) {
-                const unsigned kk = (s0 + t) * 16 + col;
-                const int u = __shfl(safe, kk);
-                const char* p = kbase + (u64)u * A.k_unit + (u64)((key0 + kk) & page_mask) * A.token_bytes;
-                if constexpr (kE4m3) {
+            for (int j = 0; j < K::kWords; ++j) x.v[i][j] = w[j];
+        }
+    };
+    if constexpr (kWide) {
+        const int u0 = __builtin_amdgcn_readlane(unit, at);
+        const u64 u = u0 < 0 ? 0 : u0;
+        const unsigned slot = key0 & mask;
+        const char* kb = A.k + u * A.k_unit + head_off + (u64)slot * A.token_bytes;
+        const char* vb = A.v + u * A.v_unit + head_off + (u64)slot * A.token_bytes;
+        const unsigned tb = (unsigned)A.token_bytes;
+        k_from(kb + p.col * tb);
 #pragma unroll
-                    for (int f = 0; f < kFrags; f += 2) {
-                        const u32x4 c = *reinterpret_cast<const u32x4*>(p + (kdim[f] < A.dim ? kdim[f] : 0));
-                        kf[t][f] = u32x4{T::template from_e4m3<false>(c[0]), T::template from_e4m3<true>(c[0]),
-                                         T::template from_e4m3<false>(c[1]), T::template from_e4m3<true>(c[1])};
-                        kf[t][f + 1] = u32x4{T::template from_e4m3<false>(c[2]), T::template from_e4m3<true>(c[2]),
-                                             T::template from_e4m3<false>(c[3]), T::template from_e4m3<true>(c[3])};
-                    }
-                } else {
+        for (int i = 0; i < 4; ++i) v_from(vb + ((4 * p.quad + i) * tb + p.vd), i);
+        if constexpr (kE4m3) {
+            const u64 so = A.scale_off + 4 * (((u64)head << A.shift) + slot);
+            x.ks = *reinterpret_cast<const f32x4*>(A.k + u * A.k_unit + so + 16 * p.quad);
+            x.vs = *reinterpret_cast<const f32x4*>(A.v + u * A.v_unit + so + 16 * p.quad);
+        }
+    } else {
+        const int safe = unit < 0 ? 0 : unit;
+        const u64 ku = (u64)__shfl(safe, at + p.col);
+        k_from(A.k + ku * A.k_unit + head_off + (u64)((key0 + p.col) & mask) * A.token_bytes);
 #pragma unroll
-                    for (int f = 0; f < kFrags; ++f)
-                        kf[t][f] = *reinterpret_cast<const u32x4*>(p + 2 * (kdim[f] < A.dim ? kdim[f] : 0));
-                }
-                if (A.dim != kDim) {
-#pragma unroll
-                    for (int f = 0; f < kFrags; ++f)
-                        if (kdim[f] >= A.dim) kf[t][f] = u32x4{0, 0, 0, 0};
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const unsigned vk = (s0 + t) * 16 + 4 * quad + i;
-                    const int vu = __shfl(safe, vk);
-                    const unsigned slot = (key0 + vk) & page_mask;
-                    vo[t][i] = (u64)vu * A.v_unit;
-                    const char* vp = vbase + vo[t][i] + (u64)slot * A.token_bytes + vdim * (kE4m3 ? 1 : 2);
-                    if constexpr (kE4m3) {
-                        const u64 so = A.scale_off + 4 * (((u64)head << A.shift) + slot);
-                        kscale[t][i] = *reinterpret_cast<const float*>(A.k + (u64)vu * A.k_unit + so);
-                        vscale[t][i] = *reinterpret_cast<const float*>(A.v + vo[t][i] + so);
-                        unsigned c[kCols / 4];
-#pragma unroll
-                        for (int w = 0; w < kCols / 4; ++w) c[w] = reinterpret_cast<const unsigned*>(vp)[w];
-#pragma unroll
-                        for (int w = 0; w < kCols / 4; ++w) {
-                            vr[t][i][2 * w] = P::template from_e4m3<false>(c[w]);
-                            vr[t][i][2 * w + 1] = P::template from_e4m3<true>(c[w]);
-                        }
-                    } else {
-                        typedef unsigned wide __attribute__((ext_vector_type(kCols / 2)));
-                        const wide c = *reinterpret_cast<const wide*>(vp);
-#pragma unroll
-                        for (int w = 0; w < kCols / 2; ++w) vr[t][i][w] = c[w];
-                    }
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < kSub; ++t) {
-                st[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int f = 0; f < kFrags; ++f) st[t] = T::mma(kf[t][f], qf[f], st[t]);
-            }
-            float best = top;
-#pragma unroll
-            for (int t = 0; t < kSub; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = st[t][i] * A.scale;
-                    if constexpr (kE4m3) x *= kscale[t][i];
-                    const unsigned kk = (s0 + t) * 16 + 4 * quad + i;
-                    const bool seen = (there >> kk & 1) && (!own || (int)(key0 + kk) < lim);
-                    sc[t][i] = seen ? x : -INFINITY;
-                    best = fmaxf(best, sc[t][i]);
-                }
-            best = fmaxf(best, __shfl_xor(best, 16));
-            best = fmaxf(best, __shfl_xor(best, 32));
-            const float ref = best == -INFINITY ? 0.f : best;
-            const float shrink = exp2f(top - ref);
-            top = best;
-            sum *= shrink;
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) o[i] *= shrink;
-            unsigned pw[kSub][2];
-#pragma unroll
-            for (int t = 0; t < kSub; ++t) {
-                float w[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = exp2f(sc[t][i] - ref);
-                    sum += w[i];
-                    // a token that is away has no scale either
-                    if constexpr (kE4m3) w[i] = sc[t][i] == -INFINITY ? 0.f : w[i] * vscale[t][i];
-                }
-                pw[t][0] = P::pack(w[0], w[1]);
-                pw[t][1] = P::pack(w[2], w[3]);
-            }
-            if (there != ~0ull) {           // what is stored there may be anything
-#pragma unroll
-                for (int t = 0; t < kSub; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!(there >> ((s0 + t) * 16 + 4 * quad + i) & 1)) {
-#pragma unroll
-                            for (int w = 0; w < kCols / 2; ++w) vr[t][i][w] = 0;
-                        }
-            }
-#pragma unroll
-            for (int t = 0; t < kSub; t += 2) {
-                const u32x4 p = {pw[t][0], pw[t][1], pw[t + 1][0], pw[t + 1][1]};
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) {
-                    constexpr unsigned kLow = 0x05040100u, kHigh = 0x07060302u;
-                    const unsigned sel = i % 2 ? kHigh : kLow;
-                    const u32x4 a = {__builtin_amdgcn_perm(vr[t][1][i / 2], vr[t][0][i / 2], sel),
-                                     __builtin_amdgcn_perm(vr[t][3][i / 2], vr[t][2][i / 2], sel),
-                                     __builtin_amdgcn_perm(vr[t + 1][1][i / 2], vr[t + 1][0][i / 2], sel),
-                                     __builtin_amdgcn_perm(vr[t + 1][3][i / 2], vr[t + 1][2][i / 2], sel)};
-                    o[i] = P::mma(a, p, o[i]);
-                }
+        for (int i = 0; i < 4; ++i) {
+            const u64 vu = (u64)__shfl(safe, at + 4 * p.quad + i);
+            const unsigned slot = (key0 + 4 * p.quad + i) & mask;
+            v_from(A.v + vu * A.v_unit + head_off + (u64)slot * A.token_bytes + p.vd, i);
+            if constexpr (kE4m3) {
+                const u64 so = A.scale_off + 4 * (((u64)head << A.shift) + slot);
+                x.ks[i] = *reinterpret_cast<const float*>(A.k + vu * A.k_unit + so);
+                x.vs[i] = *reinterpret_cast<const float*>(A.v + vu * A.v_unit + so);
             }
         }
     }
+}
+
+// What is stored where no token is may be anything: values become zeros (their
+// weights are, but 0 * NaN is not).  Bit i of `there`: the lane's value i is a token.
+template <class K>
+__device__ __forceinline__ void clear_values(K& x, unsigned there) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (!(there >> i & 1)) {
+#pragma unroll
+            for (int w = 0; w < K::kWords; ++w) x.v[i][w] = 0;
+        }
+}
+
+// The unit of key `key` of a segment, -1 where there is none.
+__device__ __forceinline__ int unit_of(const AttendArgs& A, u64 first, unsigned key, unsigned limit) {
+    return key < limit ? A.tab.unit(first + (key >> A.shift)) : -1;
+}
+
+// The keys that an item reads: blocks [b0, b1) of the prefix's and the own tokens'
+// blocks, of which the tile's rows see own tokens below `most`.
+struct Range {
+    unsigned nb0, most;
+    u64 b0, b1;
+    __device__ Range(const AttendArgs& A, const Stack& s, unsigned last_row, unsigned split) {
+        most = (unsigned)min((long long)s.keys[1], max(0ll, (long long)s.see + last_row + 1));
+        nb0 = (s.keys[0] + kBlock - 1) / kBlock;
+        b0 = (u64)split * s.chunk;
+        b1 = min((u64)nb0 + (most + kBlock - 1) / kBlock, b0 + s.chunk);
+    }
+};
+
+// Queries of one tile of 16 rows: row lane % 16, in the slots of the keys.  A scale of
+// zero or less is taken into their bits, so that scores can be compared unscaled.
+template <class T, int kDim, bool kE4m3>
+__device__ __forceinline__ void load_queries(const AttendArgs& A, const Stack& s, unsigned head,
+                                             unsigned m, unsigned quad, u32x4* q) {
+    const unsigned row = m / A.per, g = m - row * A.per;
+    const bool in = m < s.rows * A.per;
+    const char* from = A.q + (u64)(s.row0 + (in ? row : 0)) * A.q_row + (u64)(head * A.per + (in ? g : 0)) * A.q_head;
+#pragma unroll
+    for (int f = 0; f < kDim / 32; ++f) {
+        const unsigned d = Keys<T, kDim, kE4m3>::slot_dim(f, quad);
+        q[f] = u32x4{0, 0, 0, 0};
+        if (in && d < A.dim) q[f] = (*reinterpret_cast<const u32x4*>(from + 2 * d) & A.q_keep) ^ A.q_flip;
+    }
+}
+
+// Running reference and sum of one row's scores, and its weights.  `top` is an
+// unscaled score; weights are 2^(scale (score - top)).
+struct Softmax {
+    float top = -INFINITY, sum = 0.f;
+    // Whether a score passes the reference by more than the slack (in some lane).
+    __device__ bool passes(float best, float scale) const {
+        return __any(best > top && !((best - top) * scale <= kSlack));
+    }
+    // Takes the largest score of the row (over the lanes that share it) as the new
+    // reference; returns what older sums shrink by.
+    __device__ float raise(float best, float scale) {
+        best = fmaxf(best, __shfl_xor(best, 16));
+        best = fmaxf(best, __shfl_xor(best, 32));
+        best = fmaxf(best, top);
+        const float shrink = top == best ? 1.f : __builtin_amdgcn_exp2f((top - best) * scale);
+        top = best;
+        sum *= shrink;
+        return shrink;
+    }
+    __device__ float offset(float scale) const { return top == -INFINITY ? 0.f : -top * scale; }
+};
+
+// log2 of the reference's scale for a part: weights are relative to 2^this.
+__device__ __forceinline__ float reference(float top, float scale) {
+    return top == -INFINITY ? -INFINITY : top * scale;
+}
+
+// 16 rows and a range of keys.  The four waves take 64-key blocks in turn, each
+// with a reference and sum of its own, and join at the end: with so few rows a key
+// is used once, so it goes from memory to registers and through the products
+// without a stop in LDS.  HBM bounds it; a wave keeps the loads of its next 16 KB in
+// flight while it computes (bf16 at dim 128: 32 keys a step).
+template <class T, int kDim, bool kE4m3, bool kWide>
+__device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, unsigned tile,
+                         unsigned split, char* lds) {
+    typedef Keys<T, kDim, kE4m3> K;
+    typedef typename K::P P;
+    constexpr int kCols = K::kCols, kFrags = K::kFrags;
+    constexpr int kSub = kDim == 64 ? 4 : 2;            // 16-key pieces of a step
+    constexpr unsigned kSteps = 4 / kSub;               // steps of a block
+    float* lds_o = reinterpret_cast<float*>(lds);
+    float2* lds_ml = reinterpret_cast<float2*>(lds + kWaves * 16 * (kDim + 4) * 4);
+    const Places<T, kDim, kE4m3> p(A);
+    const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned col = p.col, quad = p.quad;
+    const unsigned total = s.rows * A.per;
+    const unsigned m = tile * 16 + col;                     // this lane's stack row
+    const unsigned row = m / A.per, g = m - row * A.per;
+    const unsigned last = min(total - 1, tile * 16 + 15) / A.per;
+    const Range range(A, s, last, split);
+    // own tokens that this lane's row sees
+    const int lim = (int)min((long long)s.keys[1], max(0ll, (long long)s.see + row + 1));
+    const unsigned row_first = tile * 16 / A.per;
+    const unsigned lim_all = (unsigned)min((long long)s.keys[1], max(0ll, (long long)s.see + row_first + 1));
+    u32x4 q[kFrags];
+    load_queries<T, kDim, kE4m3>(A, s, head, m, quad, q);
+    const float scale = A.scale;
+    f32x4 o[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) o[i] = f32x4{0, 0, 0, 0};
+    Softmax soft;
+
+    const u64 blocks = range.b1 > range.b0 + wave ? (range.b1 - range.b0 - wave + kWaves - 1) / kWaves : 0;
+    const u64 steps = blocks * kSteps;
+    // step i: its segment's first entry, first key, number of keys
+    auto where = [&](u64 i, bool* own, unsigned* key0) {
+        const u64 b = range.b0 + wave + i / kSteps * kWaves;
+        *own = b >= range.nb0;
+        *key0 = (unsigned)(*own ? b - range.nb0 : b) * kBlock + (unsigned)(i % kSteps) * (16 * kSub);
+    };
+    auto look_up = [&](u64 i) {
+        bool own;
+        unsigned key0;
+        where(i, &own, &key0);
+        return unit_of(A, own ? s.first[1] : s.first[0], key0 + lane % (16 * kSub),
+                       own ? range.most : s.keys[0]);
+    };
+    struct Step {
+        K x[kSub];
+        u64 there;
+    };
+    auto load = [&](u64 i, int unit, Step& t) {
+        bool own;
+        unsigned key0;
+        where(i, &own, &key0);
+        t.there = __ballot(unit >= 0);
+#pragma unroll
+        for (int j = 0; j < kSub; ++j)
+            load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * j, key0 + 16 * j, t.x[j]);
+    };
+    auto compute = [&](u64 i, Step& t) {
+        bool own;
+        unsigned key0;
+        where(i, &own, &key0);
+        f32x4 st[kSub];
+#pragma unroll
+        for (int j = 0; j < kSub; ++j) {
+            st[j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) {
+                u32x4 kf = t.x[j].key(f);
+                if (A.dim != kDim && K::slot_dim(f, quad) >= A.dim) kf = u32x4{0, 0, 0, 0};
+                st[j] = T::mma(kf, q[f], st[j]);
+            }
+            if constexpr (kE4m3) st[j] *= t.x[j].ks;
+        }
+        const u64 all = kSub == 4 ? ~0ull : (1ull << (16 * kSub)) - 1;
+        if ((t.there & all) != all || (own && key0 + 16 * kSub > lim_all)) {
+#pragma unroll
+            for (int j = 0; j < kSub; ++j) {
+                const unsigned bits = (unsigned)(t.there >> (16 * j + 4 * quad)) & 15u;
+                clear_values(t.x[j], bits);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (!(bits >> c & 1) || (own && (int)(key0 + 16 * j + 4 * quad + c) >= lim)) {
+                        st[j][c] = -INFINITY;
+                        if constexpr (kE4m3) t.x[j].vs[c] = 0.f;
+                    }
+            }
+        }
+        float best = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kSub; ++j)
+            best = fmaxf(fmaxf(fmaxf(best, st[j][0]), fmaxf(st[j][1], st[j][2])), st[j][3]);
+        if (soft.passes(best, scale)) {
+            const float shrink = soft.raise(best, scale);
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) o[c] *= shrink;
+        }
+        const float off = soft.offset(scale);
+        unsigned w[kSub][2];
+#pragma unroll
+        for (int j = 0; j < kSub; ++j) {
+            f32x4 e;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                e[c] = __builtin_amdgcn_exp2f(fmaf(st[j][c], scale, off));
+                soft.sum += e[c];
+            }
+            if constexpr (kE4m3) e *= t.x[j].vs;
+            w[j][0] = P::pack(e[0], e[1]);
+            w[j][1] = P::pack(e[2], e[3]);
+        }
+#pragma unroll
+        for (int j = 0; j < kSub; j += 2) {
+            const u32x4 pf = {w[j][0], w[j][1], w[j + 1][0], w[j + 1][1]};
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                const unsigned sel = c % 2 ? 0x07060302u : 0x05040100u;
+                const K &x = t.x[j], &y = t.x[j + 1];
+                const u32x4 vf = {__builtin_amdgcn_perm(x.value(1, c / 2), x.value(0, c / 2), sel),
+                                  __builtin_amdgcn_perm(x.value(3, c / 2), x.value(2, c / 2), sel),
+                                  __builtin_amdgcn_perm(y.value(1, c / 2), y.value(0, c / 2), sel),
+                                  __builtin_amdgcn_perm(y.value(3, c / 2), y.value(2, c / 2), sel)};
+                o[c] = P::mma(vf, pf, o[c]);
+            }
+        }
+    };
+    if (steps) {
+        Step a, b;
+        int unit = look_up(0);
+        load(0, unit, a);
+        unit = steps > 1 ? look_up(1) : -1;
+        for (u64 i = 0; i < steps; i += 2) {
+            if (i + 1 < steps) load(i + 1, unit, b);
+            if (i + 2 < steps) unit = look_up(i + 2);
+            compute(i, a);
+            if (i + 1 >= steps) break;
+            if (i + 2 < steps) load(i + 2, unit, a);
+            if (i + 3 < steps) unit = look_up(i + 3);
+            compute(i + 1, b);
+        }
+    }
+    float sum = soft.sum;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
+    const float top = reference(soft.top, scale);
 
     // join the four waves: lds_o[wave][row][kDim + 4], lds_ml[wave][row]
     constexpr int kPitch = kDim + 4;
     if (quad == 0) lds_ml[wave * 16 + col] = float2{top, sum};
     __syncthreads();
-    float all = -INFINITY, l = 0.f;
+    float best = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) all = fmaxf(all, lds_ml[w * 16 + col].x);
-    const float ref = all == -INFINITY ? 0.f : all;
+    for (int w = 0; w < kWaves; ++w) best = fmaxf(best, lds_ml[w * 16 + col].x);
+    const float ref = best == -INFINITY ? 0.f : best;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) l += lds_ml[w * 16 + col].y * exp2f(lds_ml[w * 16 + col].x - ref);
     const bool direct = s.part == ~0ull;
-    const float mine = exp2f(top - ref) * (direct ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f);
+    const float mine = exp2f(top - ref) * (direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -456,7 +614,7 @@ __device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, uns
     const u64 part0 = s.part + ((u64)head * s.splits + split) * total;
     for (unsigned e = threadIdx.x; e < 16 * (kDim / 4); e += kWaves * 64) {
         const unsigned mm = e / (kDim / 4), d = e % (kDim / 4) * 4;
-        const unsigned sm = tile * kTileRows + mm;
+        const unsigned sm = tile * 16 + mm;
         if (sm >= total || d >= A.dim) continue;
         f32x4 x = {0, 0, 0, 0};
 #pragma unroll
@@ -474,21 +632,224 @@ __device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, uns
         if (direct) {
             if (A.lse)
                 A.lse[(u64)(s.row0 + row) * (A.n_heads * A.per) + head * A.per + g] =
-                    (all + log2f(l)) * 0.6931471805599453f;
+                    (best + log2f(l)) * 0.6931471805599453f;
         } else {
-            A.part_ml[part0 + m] = float2{all, l};
+            A.part_ml[part0 + m] = float2{best, l};
         }
     }
     __syncthreads();            // the next item's LDS
 }
 
-template <class T, int kDim, bool kE4m3>
+// 64 kQ rows and a range of keys: each wave has 16 kQ rows and all keys.  A block of
+// 64 keys and values goes through LDS once for the four waves, in the layout of the
+// products' operands (a fragment is 64 lanes x 16 bytes, so neither side has bank
+// conflicts); wave w brings the block's keys 16 w .. 16 w + 15, converted and
+// transposed on the way, while the products of the block before run.  From about
+// 150 rows on the products bound it, below HBM does.
+template <class T, int kDim, bool kE4m3, bool kWide, int kQ>
+__device__ void many_rows(const AttendArgs& A, const Stack& s, unsigned head, unsigned tile,
+                          unsigned split, char* lds) {
+    typedef Keys<T, kDim, kE4m3> K;
+    typedef typename K::P P;
+    constexpr int kCols = K::kCols, kFrags = K::kFrags;
+    constexpr unsigned kKeyBytes = 4 * kFrags * 1024, kValueBytes = 2 * kCols * 1024;
+    constexpr unsigned kBuffer = kKeyBytes + kValueBytes + 512;
+    const Places<T, kDim, kE4m3> p(A);
+    const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned col = p.col, quad = p.quad;
+    const unsigned total = s.rows * A.per;
+    const unsigned m0 = tile * 64 * kQ, mw = m0 + wave * 16 * kQ;   // the tile's, the wave's first row
+    const unsigned last = min(total - 1, m0 + 64 * kQ - 1) / A.per;
+    const Range range(A, s, last, split);
+    int lim[kQ];
+    u32x4 q[kQ][kFrags];
+    f32x4 o[kQ][kCols];
+    Softmax soft[kQ];
+#pragma unroll
+    for (int t = 0; t < kQ; ++t) {
+        const unsigned m = mw + 16 * t + col;
+        lim[t] = (int)min((long long)s.keys[1], max(0ll, (long long)s.see + m / A.per + 1));
+        load_queries<T, kDim, kE4m3>(A, s, head, m, quad, q[t]);
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) o[t][i] = f32x4{0, 0, 0, 0};
+    }
+    // own tokens that all rows of the wave see
+    const unsigned lim_all = (unsigned)min((long long)s.keys[1],
+                                           max(0ll, (long long)s.see + mw / A.per + 1));
+    const float scale = A.scale;
+    auto look_up = [&](u64 b) {
+        const bool own = b >= range.nb0;
+        return unit_of(A, own ? s.first[1] : s.first[0], (unsigned)(own ? b - range.nb0 : b) * kBlock + lane,
+                       own ? range.most : s.keys[0]);
+    };
+    K x;
+    auto load = [&](u64 b, int unit) {
+        const unsigned key0 = (unsigned)(b >= range.nb0 ? b - range.nb0 : b) * kBlock;
+        load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * wave, key0 + 16 * wave, x);
+    };
+    int unit = -1, next = -1;
+    if (range.b0 < range.b1) {
+        next = look_up(range.b0);
+        load(range.b0, next);
+    }
+    unsigned buffer = 0;
+    for (u64 b = range.b0; b < range.b1; ++b, buffer ^= 1) {
+        unit = next;
+        if (b + 1 < range.b1) next = look_up(b + 1);
+        const u64 there = __ballot(unit >= 0);
+        char* const lk = lds + buffer * kBuffer;
+        char* const lv = lk + kKeyBytes;
+        float* const ls = reinterpret_cast<float*>(lv + kValueBytes);
+        if (there != ~0ull) {
+            const unsigned bits = (unsigned)(there >> (16 * wave + 4 * quad)) & 15u;
+            clear_values(x, bits);
+            if constexpr (kE4m3) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (!(bits >> c & 1)) x.ks[c] = x.vs[c] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+            u32x4 kf = x.key(f);
+            if (A.dim != kDim && K::slot_dim(f, quad) >= A.dim) kf = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4*>(lk + ((wave * kFrags + f) * 64 + lane) * 16) = kf;
+        }
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            const unsigned sel = c % 2 ? 0x07060302u : 0x05040100u;
+            const u32x2 vf = {__builtin_amdgcn_perm(x.value(1, c / 2), x.value(0, c / 2), sel),
+                              __builtin_amdgcn_perm(x.value(3, c / 2), x.value(2, c / 2), sel)};
+            *reinterpret_cast<u32x2*>(lv + (((wave / 2) * kCols + c) * 64 + lane) * 16 + (wave % 2) * 8) = vf;
+        }
+        if constexpr (kE4m3) {
+            if (col == 0) {
+                *reinterpret_cast<f32x4*>(ls + 16 * wave + 4 * quad) = x.ks;
+                *reinterpret_cast<f32x4*>(ls + 64 + 16 * wave + 4 * quad) = x.vs;
+            }
+        }
+        __syncthreads();
+        if (b + 1 < range.b1) load(b + 1, next);
+        // scores
+        f32x4 st[kQ][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int t = 0; t < kQ; ++t) st[t][j] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) {
+                const u32x4 kf = *reinterpret_cast<const u32x4*>(lk + ((j * kFrags + f) * 64 + lane) * 16);
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) st[t][j] = T::mma(kf, q[t][f], st[t][j]);
+            }
+            if constexpr (kE4m3) {
+                const f32x4 ks = *reinterpret_cast<const f32x4*>(ls + 16 * j + 4 * quad);
+#pragma unroll
+                for (int t = 0; t < kQ; ++t) st[t][j] *= ks;
+            }
+        }
+        const bool own = b >= range.nb0;
+        const unsigned key0 = (unsigned)(own ? b - range.nb0 : b) * kBlock;
+        if (there != ~0ull || (own && key0 + kBlock > lim_all)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned bits = (unsigned)(there >> (16 * j + 4 * quad)) & 15u;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int t = 0; t < kQ; ++t)
+                        if (!(bits >> c & 1) || (own && (int)(key0 + 16 * j + 4 * quad + c) >= lim[t]))
+                            st[t][j][c] = -INFINITY;
+            }
+        }
+        unsigned w[kQ][4][2];
+#pragma unroll
+        for (int t = 0; t < kQ; ++t) {
+            float best = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                best = fmaxf(fmaxf(fmaxf(best, st[t][j][0]), fmaxf(st[t][j][1], st[t][j][2])), st[t][j][3]);
+            if (soft[t].passes(best, scale)) {
+                const float shrink = soft[t].raise(best, scale);
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) o[t][c] *= shrink;
+            }
+            const float off = soft[t].offset(scale);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f32x4 e;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    e[c] = __builtin_amdgcn_exp2f(fmaf(st[t][j][c], scale, off));
+                    soft[t].sum += e[c];
+                }
+                if constexpr (kE4m3) e *= *reinterpret_cast<const f32x4*>(ls + 64 + 16 * j + 4 * quad);
+                w[t][j][0] = P::pack(e[0], e[1]);
+                w[t][j][1] = P::pack(e[2], e[3]);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                const u32x4 vf = *reinterpret_cast<const u32x4*>(lv + ((h * kCols + c) * 64 + lane) * 16);
+#pragma unroll
+                for (int t = 0; t < kQ; ++t)
+                    o[t][c] = P::mma(vf, u32x4{w[t][2 * h][0], w[t][2 * h][1], w[t][2 * h + 1][0],
+                                               w[t][2 * h + 1][1]}, o[t][c]);
+            }
+    }
+    const bool direct = s.part == ~0ull;
+    const u64 part0 = s.part + ((u64)head * s.splits + split) * total;
+#pragma unroll
+    for (int t = 0; t < kQ; ++t) {
+        const unsigned m = mw + 16 * t + col;
+        float sum = soft[t].sum;
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        const float top = reference(soft[t].top, scale);
+        if (m >= total) continue;
+        const unsigned row = m / A.per, hh = head * A.per + (m - row * A.per);
+        const float mine = direct ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+        char* to = A.out + (u64)(s.row0 + row) * A.out_row + (u64)hh * A.out_head;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const unsigned d = (4 * quad + r) * kCols;
+            if (d >= A.dim) continue;
+#pragma unroll
+            for (int c = 0; c < kCols; c += 4) {
+                const f32x4 y = f32x4{o[t][c][r], o[t][c + 1][r], o[t][c + 2][r], o[t][c + 3][r]} * mine;
+                if (direct)
+                    *reinterpret_cast<u32x2*>(to + 2 * (d + c)) = u32x2{T::pack(y[0], y[1]), T::pack(y[2], y[3])};
+                else
+                    *reinterpret_cast<f32x4*>(&A.part_o[(part0 + m) * kDim + d + c]) = y;
+            }
+        }
+        if (quad == 0) {
+            if (direct) {
+                if (A.lse) A.lse[(u64)(s.row0 + row) * (A.n_heads * A.per) + hh] =
+                    (top + log2f(sum)) * 0.6931471805599453f;
+            } else {
+                A.part_ml[part0 + m] = float2{top, sum};
+            }
+        }
+    }
+    __syncthreads();            // the next item's LDS
+}
+
+template <class T, int kDim, bool kE4m3, bool kWide>
 __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(AttendArgs A) {
-    __shared__ __align__(16) float s_o[kWaves * 16 * (kDim + 4)];
-    __shared__ float2 s_ml[kWaves * 16];
-    const u64 n = (u64)*A.n_items * A.n_heads;
+    // two buffers of a block's keys, values and scales, or the waves' sums
+    constexpr int kBlocks = 2 * (kDim * 256 + 512), kSums = kWaves * 16 * (kDim + 4) * 4 + kWaves * 16 * 8;
+    __shared__ __align__(16) char lds[kBlocks > kSums ? kBlocks : kSums];
+    __shared__ unsigned s_ticket[2];
+    const u64 n = (u64)A.n_items[0] * A.n_heads;
     const unsigned stacks = A.n_requests + A.n_groups;
-    for (u64 it = blockIdx.x; it < n; it += gridDim.x) {
+    // Items are taken as workgroups get free.  Which workgroup computes an item
+    // changes nothing in its result.  The next one is asked for early.
+    u64 it = blockIdx.x;
+    for (unsigned turn = 0; it < n; turn ^= 1) {
+        if (threadIdx.x == 0) s_ticket[turn] = gridDim.x + atomicAdd(&A.n_items[2], 1u);
         const unsigned entry = (unsigned)(it / A.n_heads), head = (unsigned)(it % A.n_heads);
         // stacks without items share their first item with the next one, which
         // is the one that the search gives
@@ -496,8 +857,16 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
         const Stack s = A.stacks[si];
         const unsigned local = entry - A.item0[si];
         const unsigned tiles = (unsigned)tiles_of(A, s);
-        if (s.splits == 0 || local >= tiles * s.splits) continue;
-        few_rows<T, kDim, kE4m3>(A, s, head, local % tiles, local / tiles, s_o, s_ml);
+        if (s.splits != 0 && local < tiles * s.splits) {
+            const unsigned tile = local % tiles, split = local / tiles;
+            const unsigned rows = tile_rows(A, s);
+            if (rows == 16) few_rows<T, kDim, kE4m3, kWide>(A, s, head, tile, split, lds);
+            else if (rows == 64) many_rows<T, kDim, kE4m3, kWide, 1>(A, s, head, tile, split, lds);
+            else many_rows<T, kDim, kE4m3, kWide, 2>(A, s, head, tile, split, lds);
+        } else {
+            __syncthreads();
+        }
+        it = s_ticket[turn];
     }
 }
 
@@ -538,7 +907,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
                 x[c] = x[c] * a + (lane * kCols + c < A.dim ? p[c] * b : 0.f);
         }
     }
-    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     char* to = A.out + (u64)t * A.out_row + (u64)qh * A.out_head;
 #pragma unroll
     for (int c = 0; c < kCols; ++c)
@@ -555,7 +924,7 @@ u64 up(u64 x) { return (x + 255) & ~255ull; }
 // prefix, and a tile for each split beyond a stack's first; there are at most
 // kTarget of those, as every one but a stack's last has its share of the work.
 u64 part_rows(u64 n_rows, u64 n_q_heads) {
-    return 2 * n_rows * n_q_heads + (u64)kTarget * kTileRows;
+    return 2 * n_rows * n_q_heads + (u64)kTarget * kMostRows;
 }
 
 struct Layout {
@@ -575,8 +944,9 @@ Layout layout_of(u64 n_rows, u64 n_requests, u64 n_groups, u64 n_q_heads, unsign
 template <class T, int kDim, bool kE4m3>
 void attend_launch(const AttendArgs& A, unsigned cus, hipStream_t st) {
     hipLaunchKernelGGL(k_attend_plan, dim3(1), dim3(kPlanThreads), 0, st, A);
-    hipLaunchKernelGGL((k_attend<T, kDim, kE4m3>), dim3(cus * (kDim > 128 ? 1 : 2)), dim3(kWaves * 64),
-                       0, st, A);
+    const dim3 grid(cus * (kDim > 128 ? 1 : 2)), block(kWaves * 64);
+    if (A.shift >= 4) hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, true>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, false>), grid, block, 0, st, A);
     const u64 waves = (u64)A.n_rows * A.n_heads * A.per;
     hipLaunchKernelGGL((k_attend_join<T, kDim>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, A);
 }
@@ -683,7 +1053,9 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     A.per = n_q_heads / cache->n_heads;
     A.dim = dim;
     A.shift = (unsigned)__builtin_ctz(cache->page_tokens);
-    A.scale = scale * 1.4426950408889634f;
+    A.scale = scale == 0.f ? 1.f : fabsf(scale) * 1.4426950408889634f;
+    A.q_keep = scale == 0.f ? 0u : ~0u;
+    A.q_flip = scale < 0.f ? 0x80008000u : 0u;
     char* ws = static_cast<char*>(workspace);
     A.n_items = reinterpret_cast<unsigned*>(ws);
     A.item0 = reinterpret_cast<unsigned*>(ws + l.item0);

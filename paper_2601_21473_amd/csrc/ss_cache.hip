@@ -277,6 +277,7 @@ ss_status cache_args(const ss_kv_cache* c, uint32_t row_type) {
     if (c->type == SS_E4M3 && c->scale_off < page_bytes(c))
         return set_err(SS_ERR_ARG, "scale_off lies inside the page's codes");
     const u64 span = unit_span(c);
+    if (span >= (1ull << 31)) return set_err(SS_ERR_ARG, "a page is too large (2^31 bytes)");
     if (c->capacity_units > 1 && (c->k_unit_bytes < span || c->v_unit_bytes < span))
         return set_err(SS_ERR_ARG, "a page of %llu bytes does not fit into a unit's chunk",
                        (unsigned long long)span);

@@ -78,6 +78,7 @@ CACHES = [
     (dict(type=B.SS_E4M3, token_bytes=64, head_bytes=1024, scale_off=2032), "inside the page"),
     (dict(type=B.SS_E4M3, token_bytes=64, head_bytes=1024, scale_off=16384), "does not fit"),
     (dict(k_unit_bytes=1 << 62), "too large"), (dict(token_bytes=1 << 63, head_bytes=128), "does not fit|large"),
+    (dict(capacity_units=1, token_bytes=1 << 28, head_bytes=128), "too large"),
 ]
 
 
