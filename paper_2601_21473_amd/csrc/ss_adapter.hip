@@ -18,9 +18,9 @@ namespace ss {
 
 namespace {
 
-constexpr int kTile = 16;               // rows of a tile
+constexpr unsigned kTile = 16;          // rows of a tile of k_adapter_in
 constexpr int kThreads = 256;
-constexpr int kOutCols = 256;           // columns of out per workgroup
+constexpr unsigned kOutCols = 512;      // columns of out per workgroup, 128 a wave
 
 struct AdapterArgs {
     Table tab;
@@ -40,9 +40,10 @@ struct AdapterArgs {
     unsigned pieces, piece;             // pieces of n_in, and elements of one
 };
 
-// Tile i of the batch: request r's tiles begin at row_off[r] / 16 + r, which leaves
+// Tile i of the batch: request r's tiles begin at row_off[r] / kTile + r, which leaves
 // room for every request's last, partly filled tile without a pass over the offsets.
 // Returns the tile's rows (0: no such tile).
+template <unsigned kTile>
 __device__ inline unsigned tile_of(const AdapterArgs& A, unsigned i, unsigned* r, unsigned* row0) {
     *r = wave_search(A.n_requests, i, [&](unsigned j) {
         const u64 s = (u64)A.row_off[j] / kTile + j;
@@ -69,7 +70,7 @@ template <class T, int kTiles>
 __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
     __shared__ __align__(16) f32x4 s_acc[3][kTiles][64];
     unsigned r, row0;
-    const unsigned rows = tile_of(A, blockIdx.x / A.pieces, &r, &row0), piece = blockIdx.x % A.pieces;
+    const unsigned rows = tile_of<kTile>(A, blockIdx.x / A.pieces, &r, &row0), piece = blockIdx.x % A.pieces;
     if (!rows) return;
     const int unit = adapter_of(A, r);
     if (unit < 0) return;
@@ -116,119 +117,175 @@ __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
     }
 }
 
-// A workgroup per tile and kOutCols columns.  A x enters as two 16-bit parts, the rounded value and
-// what the rounding left, next to each other along the summed index (the columns of
-// B are read for both), so that its 32 bits count for 16 (bf16) or 22 (fp16) of
-// them.  For fp16 each row is first divided by a power of two near its largest
-// value, as sums can pass that type's range.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_adapter_out(AdapterArgs A) {
-    __shared__ __align__(16) unsigned short s_h[kTile][2 * 128 + 8];    // two parts, zeros behind
-    __shared__ float s_scale[kTile];
-    __shared__ __align__(16) float s_y[kTile][kOutCols + 4];
+// A workgroup per tile of up to 16 kSub rows and kOutCols columns; a wave takes 128 of
+// them.  A x enters as two 16-bit parts, the rounded value and what the rounding left,
+// so that its 32 bits count for 16 (bf16) or 22 (fp16) of them; for fp16 each row is
+// first divided by a power of two near its largest value, as sums can pass that type's
+// range.  Up to rank 16 both parts fit next to each other into one product's 32 summed
+// indices, and the rows of B are read for both.
+// Column n0 + 8 (lane % 16) + j is that of product j, so a lane ends up with eight
+// columns next to each other of four rows and moves them in 16 bytes, with nothing
+// exchanged.  HBM bounds it: base and B are asked for before the wait for A x.
+template <class T, int kSub, bool kPacked>
+__global__ __launch_bounds__(kThreads, kSub == 1 ? 4 : 2) void k_adapter_out(AdapterArgs A) {
+    constexpr unsigned kRows = 16 * kSub, kPitch = kPacked ? 40 : 2 * 128 + 8;
+    __shared__ __align__(16) unsigned short s_h[kRows][kPitch];     // two parts, zeros behind
+    __shared__ float s_scale[kRows];
     unsigned r, row0;
     const unsigned parts = (A.n_out + kOutCols - 1) / kOutCols;
-    const unsigned rows = tile_of(A, blockIdx.x / parts, &r, &row0);
+    const unsigned rows = tile_of<kRows>(A, blockIdx.x / parts, &r, &row0);
     if (!rows) return;
     const int unit = adapter_of(A, r);
+    if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned col = lane % 16, quad = lane / 16;
-    const unsigned n0 = blockIdx.x % parts * kOutCols;
-    const unsigned slots = (2 * A.rank + 31) & ~31u;
+    const unsigned n = blockIdx.x % parts * kOutCols + wave * 128 + 8 * col;    // first of eight
+    const bool in = n < A.n_out;
+    const u64 out_at = (u64)n * 2;
+    // the first 16 rows' share of base, and B for the first 32 ranks
+    u32x4 base[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned t = 4 * quad + i;
+        base[i] = u32x4{0, 0, 0, 0};
+        if (in && t < rows)
+            base[i] = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + out_at);
+    }
+    const unsigned rank8 = A.rank / 8;
+    const char* const bm = A.b + (u64)(unit < 0 ? 0 : unit) * A.b_unit + (u64)(in ? n : 0) * A.rank * 2;
+    // eight ranks of the lane's column j in step k: packed, ranks and parts go round
+    auto load_b = [&](unsigned k, u32x4* b) {
+        const unsigned c = 4 * k + quad, from = kPacked && c >= rank8 ? c - rank8 : c;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            b[j] = u32x4{0, 0, 0, 0};
+            if (from < rank8) b[j] = *reinterpret_cast<const u32x4*>(bm + ((u64)j * rank8 + from) * 16);
+        }
+    };
+    u32x4 bf[8];
+    if (unit >= 0) load_b(0, bf);
     if (unit >= 0) {
         // 16 lanes a row: eight ranks each
-        const unsigned i = threadIdx.x / 16, c = threadIdx.x % 16 * 8;
-        float h[8], top = 0.f;
+        for (unsigned i0 = 0; i0 < kRows; i0 += 16) {
+            const unsigned i = i0 + threadIdx.x / 16, c = threadIdx.x % 16 * 8;
+            float h[8], top = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) h[j] = 0.f;
-        if (i < rows && c < A.rank)
-            for (unsigned p = 0; p < A.pieces; ++p) {
-                const float* from = A.low + ((u64)p * A.n_rows + row0 + i) * A.rank + c;
-                const f32x4 u = *reinterpret_cast<const f32x4*>(from);
-                const f32x4 v = *reinterpret_cast<const f32x4*>(from + 4);
+            for (int j = 0; j < 8; ++j) h[j] = 0.f;
+            if (i < rows && c < A.rank)
+#pragma unroll 2
+                for (unsigned p = 0; p < A.pieces; ++p) {
+                    const float* from = A.low + ((u64)p * A.n_rows + row0 + i) * A.rank + c;
+                    const f32x4 u = *reinterpret_cast<const f32x4*>(from);
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(from + 4);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    h[j] += u[j];
-                    h[4 + j] += v[j];
+                    for (int j = 0; j < 4; ++j) {
+                        h[j] += u[j];
+                        h[4 + j] += v[j];
+                    }
+                }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(h[j]));
+#pragma unroll
+            for (int m = 8; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+            float unscale = 1.f;
+            if constexpr (std::is_same<T, F16>::value) {
+                if (top > 0.f && top < INFINITY) {
+                    const int e = min(max(ilogbf(top), -100), 100);
+                    unscale = ldexpf(1.f, e);
+                    const float s = ldexpf(1.f, -e);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[j] *= s;
                 }
             }
+            if (c == 0) s_scale[i] = unscale * (A.scales ? A.scales[r] : 1.f);
+            unsigned hi[4], lo[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(h[j]));
-#pragma unroll
-        for (int m = 8; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-        float unscale = 1.f;
-        if constexpr (std::is_same<T, F16>::value) {
-            if (top > 0.f && top < INFINITY) {
-                const int e = min(max(ilogbf(top), -100), 100);
-                unscale = ldexpf(1.f, e);
-                const float s = ldexpf(1.f, -e);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[j] *= s;
+            for (int j = 0; j < 4; ++j) {
+                hi[j] = T::pack(h[2 * j], h[2 * j + 1]);
+                const float a = T::lo(hi[j]), b = T::hi(hi[j]);     // no rest of an infinity
+                lo[j] = T::pack(fabsf(a) < INFINITY ? h[2 * j] - a : 0.f,
+                                fabsf(b) < INFINITY ? h[2 * j + 1] - b : 0.f);
+            }
+            const u32x4 high = {hi[0], hi[1], hi[2], hi[3]}, rest = {lo[0], lo[1], lo[2], lo[3]};
+            if constexpr (kPacked) {        // ranks, their rests, zeros up to 32
+                if (c < A.rank) {
+                    *reinterpret_cast<u32x4*>(&s_h[i][c]) = high;
+                    *reinterpret_cast<u32x4*>(&s_h[i][A.rank + c]) = rest;
+                }
+                if (2 * A.rank + c < 32) *reinterpret_cast<u32x4*>(&s_h[i][2 * A.rank + c]) = u32x4{0, 0, 0, 0};
+            } else {                        // ranks up to 128, then their rests (0 behind the last)
+                *reinterpret_cast<u32x4*>(&s_h[i][c]) = high;
+                *reinterpret_cast<u32x4*>(&s_h[i][128 + c]) = rest;
             }
         }
-        if (c == 0) s_scale[i] = unscale * (A.scales ? A.scales[r] : 1.f);
-        // columns 0 .. rank: rounded values, rank .. 2 rank: the rests, then zeros
-        unsigned hi[4], lo[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            hi[j] = T::pack(h[2 * j], h[2 * j + 1]);
-            const float a = T::lo(hi[j]), b = T::hi(hi[j]);         // no rest of an infinity
-            lo[j] = T::pack(fabsf(a) < INFINITY ? h[2 * j] - a : 0.f,
-                            fabsf(b) < INFINITY ? h[2 * j + 1] - b : 0.f);
-        }
-        if (c < A.rank) {
-            *reinterpret_cast<u32x4*>(&s_h[i][c]) = u32x4{hi[0], hi[1], hi[2], hi[3]};
-            *reinterpret_cast<u32x4*>(&s_h[i][A.rank + c]) = u32x4{lo[0], lo[1], lo[2], lo[3]};
-        }
-        if (2 * A.rank + c < slots)
-            *reinterpret_cast<u32x4*>(&s_h[i][2 * A.rank + c]) = u32x4{0, 0, 0, 0};
         __syncthreads();
-        // products of 16 columns x 16 rows, four to a wave
-        f32x4 acc[4];
-        const char* br[4];
+    }
+    f32x4 acc[kSub][8];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            acc[t] = f32x4{0, 0, 0, 0};
-            const unsigned n = n0 + wave * 64 + t * 16 + col;
-            br[t] = A.b + (u64)unit * A.b_unit + (u64)(n < A.n_out ? n : 0) * A.rank * 2;
-        }
-        for (unsigned k = 0; k < slots; k += 32) {
-            const unsigned at = k + quad * 8;           // a slot of eight
-            const unsigned from = at < A.rank ? at : at - A.rank;
-            const u32x4 hf = *reinterpret_cast<const u32x4*>(&s_h[col][at]);
+    for (int t = 0; t < kSub; ++t)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                u32x4 bf = {0, 0, 0, 0};
-                if (at < 2 * A.rank) bf = *reinterpret_cast<const u32x4*>(br[t] + from * 2);
-                acc[t] = T::mma(bf, hf, acc[t]);
+        for (int j = 0; j < 8; ++j) acc[t][j] = f32x4{0, 0, 0, 0};
+    if (unit >= 0) {
+        const unsigned steps = kPacked ? 1 : (A.rank + 31) / 32;
+        for (unsigned k = 0; k < steps; ++k) {
+            u32x4 next[8];
+            if (!kPacked && k + 1 < steps) load_b(k + 1, next);
+#pragma unroll
+            for (int t = 0; t < kSub; ++t) {
+                const unsigned short* h = &s_h[16 * t + col][32 * k + 8 * quad];
+                const u32x4 high = *reinterpret_cast<const u32x4*>(h);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(high, bf[j], acc[t][j]);
+                if constexpr (!kPacked) {
+                    const u32x4 rest = *reinterpret_cast<const u32x4*>(h + 128);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(rest, bf[j], acc[t][j]);
+                }
+            }
+            if (!kPacked && k + 1 < steps) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) bf[j] = next[j];
             }
         }
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            *reinterpret_cast<f32x4*>(&s_y[col][wave * 64 + t * 16 + quad * 4]) = acc[t];
-        __syncthreads();
-    } else if (A.base == A.out) {
-        return;
     }
-    for (unsigned e = threadIdx.x; e < rows * (kOutCols / 8); e += kThreads) {
-        const unsigned i = e / (kOutCols / 8), c = e % (kOutCols / 8) * 8;
-        if (n0 + c >= A.n_out) continue;
-        const u64 at = (u64)(n0 + c) * 2;
-        u32x4 w = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + i) * A.base_row + at);
-        if (unit >= 0) {
-            const float s = s_scale[i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = T::pack(T::lo(w[j]) + s * s_y[i][c + 2 * j], T::hi(w[j]) + s * s_y[i][c + 2 * j + 1]);
+    for (int s = 0; s < kSub; ++s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned t = 16 * s + 4 * quad + i;
+            if (!in || t >= rows) continue;
+            u32x4 w = base[i];
+            if (unit >= 0) {
+                const float f = s_scale[t];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = T::pack(T::lo(w[j]) + f * acc[s][2 * j][i], T::hi(w[j]) + f * acc[s][2 * j + 1][i]);
+            }
+            *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + t) * A.out_row + out_at) = w;
         }
-        *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + i) * A.out_row + at) = w;
+        if (s + 1 < kSub) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned t = 16 * (s + 1) + 4 * quad + i;
+                if (in && t < rows)
+                    base[i] = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + out_at);
+            }
+        }
     }
+}
+
+template <class T, int kSub>
+void out_launch(const AdapterArgs& A, hipStream_t st) {
+    const unsigned tiles = A.n_rows / (16 * kSub) + A.n_requests;
+    const dim3 grid((A.n_out + kOutCols - 1) / kOutCols * tiles), block(kThreads);
+    if (A.rank <= 16) hipLaunchKernelGGL((k_adapter_out<T, kSub, true>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_adapter_out<T, kSub, false>), grid, block, 0, st, A);
 }
 
 template <class T>
 void adapter_launch(const AdapterArgs& A, hipStream_t st) {
     const unsigned tiles = A.n_rows / kTile + A.n_requests;
-    const dim3 in(A.pieces * tiles), out((A.n_out + kOutCols - 1) / kOutCols * tiles), block(kThreads);
+    const dim3 in(A.pieces * tiles), block(kThreads);
     switch ((A.rank + 15) / 16) {
         case 1: hipLaunchKernelGGL((k_adapter_in<T, 1>), in, block, 0, st, A); break;
         case 2: hipLaunchKernelGGL((k_adapter_in<T, 2>), in, block, 0, st, A); break;
@@ -236,7 +293,9 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
         case 4: hipLaunchKernelGGL((k_adapter_in<T, 4>), in, block, 0, st, A); break;
         default: hipLaunchKernelGGL((k_adapter_in<T, 8>), in, block, 0, st, A); break;
     }
-    hipLaunchKernelGGL((k_adapter_out<T>), out, block, 0, st, A);
+    // tiles of 64 rows where requests fill them: B is read a quarter as often
+    if (A.n_rows >= 32ull * A.n_requests) out_launch<T, 4>(A, st);
+    else out_launch<T, 1>(A, st);
 }
 
 // n_in is cut into pieces of at least 256 elements (two rounds of the four waves)

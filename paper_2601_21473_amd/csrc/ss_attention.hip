@@ -58,10 +58,11 @@ struct AttendArgs {
     float scale;                                // |scale| log2(e), 1 for a scale of 0
     unsigned q_keep, q_flip;                    // queries' bits that count, and that turn
     // workspace
-    unsigned* n_items;                          // items per head; 1 where the offsets are valid;
-                                                // items taken
-    unsigned* item0;                            // [stacks + 1] first item of each stack
+    unsigned* counts;                           // items per head, rows to join, items taken
+    uint4* items;                               // [most_items] stack, tile, split
+    unsigned* join0;                            // [n_requests] rows to join before each request's
     Stack* stacks;                              // [n_requests + n_groups]
+    u64 most_items;
     float* part_o;                              // [part_rows][padded dim]
     float2* part_ml;                            // [part_rows] maximum (log2), sum
     u64 part_rows;
@@ -69,36 +70,9 @@ struct AttendArgs {
 
 constexpr int kPlanThreads = 1024;
 
-// A request's group (kNone = none): groups are searched as the requests are.
-__device__ unsigned group_of(const AttendArgs& A, unsigned r) {
-    unsigned lo = 0, hi = A.n_groups;           // largest g with group_off[g] <= r
-    while (hi - lo > 1) {
-        const unsigned mid = (lo + hi) / 2;
-        if (A.group_off[mid] <= r) lo = mid;
-        else hi = mid;
-    }
-    if (hi <= lo) return kNone;
-    return A.group_off[lo] <= r && r < A.group_off[lo + 1] && A.group_off[lo + 1] <= A.n_requests
-        ? lo : kNone;
-}
-
 __device__ unsigned tokens_with_page(const AttendArgs& A, unsigned agent, unsigned len, u64* first) {
     const u64 most = (u64)A.tab.row(agent, first) << A.shift;
     return (unsigned)(len < most ? len : most);
-}
-
-// Whether the prefix of group g is read by a stack of its own: where several
-// requests share it and are so short that a tile of rows holds more than one.
-// Otherwise each request reads prefix and own tokens in one go, without parts.
-__device__ bool pooled(const AttendArgs& A, unsigned g, unsigned* row0, unsigned* rows) {
-    const unsigned b = A.group_off[g], e = A.group_off[g + 1];
-    *row0 = *rows = 0;
-    if (b >= e || e > A.n_requests) return false;
-    const unsigned r0 = A.row_off[b], r1 = A.row_off[e];
-    if (r0 >= r1 || r1 > A.n_rows) return false;
-    *row0 = r0;
-    *rows = r1 - r0;
-    return e - b > 1 && (u64)*rows * A.per < (u64)(e - b) * 64 && A.prefix_lens[g] > 0;
 }
 
 __device__ unsigned blocks_of(const Stack& s) {
@@ -110,58 +84,86 @@ __device__ unsigned tile_rows(const AttendArgs& A, const Stack& s) {
     const u64 rows = (u64)s.rows * A.per;
     return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
 }
-__device__ u64 tiles_of(const AttendArgs& A, const Stack& s) {
-    const unsigned n = tile_rows(A, s);
-    return ((u64)s.rows * A.per + n - 1) / n;
+__device__ unsigned tiles_of(const AttendArgs& A, const Stack& s) {
+    const u64 n = tile_rows(A, s);
+    return (unsigned)(((u64)s.rows * A.per + n - 1) / n);
 }
 
-__device__ Stack stack_of(const AttendArgs& A, unsigned s) {
+// The stack of group g's prefix.  It has rows (a stack of its own) where several
+// requests share the prefix and are so short that a tile of rows holds more than
+// one; otherwise each request reads prefix and own tokens in one go, without parts.
+__device__ Stack prefix_stack(const AttendArgs& A, unsigned g) {
     Stack t{};
     t.part = ~0ull;
     t.pool = kNone;
-    if (s < A.n_requests) {
-        t.row0 = A.row_off[s];
-        t.rows = request_rows(A.row_off, s, A.n_rows);
-        if (!t.rows) return t;
-        const unsigned len = A.lens[s];
-        const long long see = (long long)len - t.rows;
-        t.see = (int)(see < -1 - (long long)t.rows ? -1 - (long long)t.rows
-                                                   : see > 0x7fffffff ? 0x7fffffff : see);
-        u64 first;
-        t.keys[1] = tokens_with_page(A, A.agents[s], len, &first);
-        t.first[1] = first;
-        const unsigned g = A.n_groups ? group_of(A, s) : kNone;
-        if (g != kNone) {
-            unsigned row0, rows;
-            if (pooled(A, g, &row0, &rows)) t.pool = A.n_requests + g;
-            else t.keys[0] = tokens_with_page(A, A.prefix_agents[g], A.prefix_lens[g], &first);
-            if (t.keys[0]) t.first[0] = first;
-        }
-    } else {
-        const unsigned g = s - A.n_requests;
-        unsigned row0, rows;
-        if (!pooled(A, g, &row0, &rows)) return t;
-        t.row0 = row0;
-        t.rows = rows;
-        u64 first;
-        t.keys[0] = tokens_with_page(A, A.prefix_agents[g], A.prefix_lens[g], &first);
-        t.first[0] = first;
+    const unsigned b = A.group_off[g], e = A.group_off[g + 1];
+    u64 first;
+    const unsigned len = A.prefix_lens[g];
+    const unsigned keys = tokens_with_page(A, A.prefix_agents[g], len, &first);
+    if (b >= e || e > A.n_requests) return t;
+    const unsigned r0 = A.row_off[b], r1 = A.row_off[e];
+    t.keys[0] = keys;
+    t.first[0] = first;
+    if (r0 < r1 && r1 <= A.n_rows && e - b > 1 && (u64)(r1 - r0) * A.per < (u64)(e - b) * 64 && len) {
+        t.row0 = r0;
+        t.rows = r1 - r0;
     }
     return t;
 }
 
-// One workgroup: the stacks, how they are split, and where each one's items and
-// parts begin.  Keys are cut into pieces of about 1/kTarget of the call's work.
+// The stack of request s's own tokens (and of its prefix, where that has none).
+__device__ Stack request_stack(const AttendArgs& A, unsigned s) {
+    Stack t{};
+    t.part = ~0ull;
+    t.pool = kNone;
+    t.row0 = A.row_off[s];
+    const unsigned len = A.lens[s], agent = A.agents[s];
+    t.rows = request_rows(A.row_off, s, A.n_rows);
+    const long long see = (long long)len - t.rows;
+    t.see = (int)(see < -1 - (long long)t.rows ? -1 - (long long)t.rows
+                                               : see > 0x7fffffff ? 0x7fffffff : see);
+    u64 first;
+    t.keys[1] = tokens_with_page(A, agent, len, &first);
+    t.first[1] = first;
+    unsigned lo = 0, hi = A.n_groups;           // the largest g with group_off[g] <= s
+    while (hi - lo > 1) {
+        const unsigned mid = (lo + hi) / 2;
+        if (A.group_off[mid] <= s) lo = mid;
+        else hi = mid;
+    }
+    if (hi > lo && A.group_off[lo] <= s && s < A.group_off[lo + 1]) {
+        const Stack& p = A.stacks[A.n_requests + lo];
+        if (p.rows) {
+            t.pool = A.n_requests + lo;
+        } else {
+            t.keys[0] = p.keys[0];
+            t.first[0] = p.first[0];
+        }
+    }
+    return t;
+}
+
+// One workgroup: the stacks, how they are split, the list of items and where each
+// stack's parts begin.  Keys are cut into pieces of about 1/kTarget of the call's
+// work.  A few reads one after the other bound it, so groups come first and requests
+// look theirs up.
 __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
     __shared__ u64 s_sum[kPlanThreads / 64][3];
-    __shared__ u64 s_base[2];
+    __shared__ u64 s_base[3];
     const unsigned n = A.n_requests + A.n_groups, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     u64 work = 0, own_rows = 0, pool_rows = 0;
-    for (unsigned s = tid; s < n; s += kPlanThreads) {
-        const Stack t = stack_of(A, s);
+    for (unsigned g = tid; g < A.n_groups; g += kPlanThreads) {
+        const Stack t = prefix_stack(A, g);
+        A.stacks[A.n_requests + g] = t;
+        work += (u64)tiles_of(A, t) * blocks_of(t);
+        pool_rows += t.rows;
+    }
+    __syncthreads();
+    for (unsigned s = tid; s < A.n_requests; s += kPlanThreads) {
+        const Stack t = request_stack(A, s);
         A.stacks[s] = t;
-        work += tiles_of(A, t) * blocks_of(t);
-        (s < A.n_requests ? own_rows : pool_rows) += t.rows;
+        work += (u64)tiles_of(A, t) * blocks_of(t);
+        own_rows += t.rows;
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) {
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
         s_sum[wave][1] = own_rows;
         s_sum[wave][2] = pool_rows;
     }
-    if (tid < 2) s_base[tid] = 0;
+    if (tid < 3) s_base[tid] = 0;
     __syncthreads();
     work = own_rows = pool_rows = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) {
@@ -186,61 +188,72 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
     const bool valid = own_rows <= A.n_rows && pool_rows <= A.n_rows;
     const u64 even = (work * A.n_heads + kTarget - 1) / kTarget;
     const unsigned chunk = (unsigned)(even > kMinBlocks ? (even < kNone ? even : kNone) : kMinBlocks);
-    for (unsigned s0 = 0; s0 < n; s0 += kPlanThreads) {
-        const unsigned s = s0 + tid;
+    for (unsigned s0 = 0; valid && s0 < n; s0 += kPlanThreads) {
+        // prefixes first: their items are the longest
+        const unsigned i = s0 + tid;
+        const unsigned s = i < A.n_groups ? A.n_requests + i : i - A.n_groups;
         Stack t{};
-        u64 items = 0, parts = 0;
-        if (s < n && valid) {
+        u64 items = 0, parts = 0, joins = 0;
+        if (i < n) {
             t = A.stacks[s];
             const unsigned blocks = blocks_of(t);
             t.chunk = chunk;
             t.splits = (unsigned)(((u64)blocks + chunk - 1) / chunk);
-            if (s < A.n_requests && t.pool == kNone && t.splits == 0) t.splits = 1;  // writes zeros
+            const bool own = s < A.n_requests;
+            if (own && t.pool == kNone && t.splits == 0) t.splits = 1;      // writes zeros
             if (!t.rows) t.splits = 0;
-            items = tiles_of(A, t) * t.splits;
-            if (t.splits > 1 || t.pool != kNone || s >= A.n_requests)
-                parts = (u64)t.rows * A.per * A.n_heads * t.splits;
+            items = (u64)tiles_of(A, t) * t.splits;
+            const bool joined = t.splits > 1 || t.pool != kNone;
+            if (joined || !own) parts = (u64)t.rows * A.per * A.n_heads * t.splits;
+            if (joined && own) joins = t.rows;
         }
         // exclusive sums over the workgroup, carried from one thousand to the next
-        u64 a = items, b = parts;
+        u64 a = items, b = parts, c = joins;
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
-            const u64 x = __shfl_up(a, m), y = __shfl_up(b, m);
+            const u64 x = __shfl_up(a, m), y = __shfl_up(b, m), z = __shfl_up(c, m);
             if (lane >= (unsigned)m) {
                 a += x;
                 b += y;
+                c += z;
             }
         }
         __syncthreads();
         if (lane == 63) {
             s_sum[wave][0] = a;
             s_sum[wave][1] = b;
+            s_sum[wave][2] = c;
         }
         __syncthreads();
-        u64 at = s_base[0] + a - items, part = s_base[1] + b - parts;
+        u64 at = s_base[0] + a - items, part = s_base[1] + b - parts, join = s_base[2] + c - joins;
         for (unsigned w = 0; w < wave; ++w) {
             at += s_sum[w][0];
             part += s_sum[w][1];
+            join += s_sum[w][2];
         }
-        if (s < n) {
-            if (parts) t.part = part + parts <= A.part_rows ? part : 0;
+        if (i < n) {
+            if (parts) t.part = part;
             A.stacks[s] = t;
-            A.item0[s] = (unsigned)at;
+            if (s < A.n_requests) A.join0[s] = (unsigned)join;
+            const unsigned tiles = tiles_of(A, t);
+            if (at + items <= A.most_items)
+                for (unsigned j = 0; j < (unsigned)items; ++j)
+                    A.items[at + j] = uint4{s, j % tiles, j / tiles, 0};
         }
         __syncthreads();
         if (tid == kPlanThreads - 1) {
             s_base[0] = at + items;
             s_base[1] = part + parts;
+            s_base[2] = join + joins;
         }
         __syncthreads();
     }
     if (tid == 0) {
-        // more parts than the workspace holds cannot be for valid offsets
-        const bool fits = s_base[1] <= A.part_rows && s_base[0] < kNone;
-        A.item0[n] = fits ? (unsigned)s_base[0] : 0;
-        A.n_items[0] = fits ? (unsigned)s_base[0] : 0;
-        A.n_items[1] = fits && valid;
-        A.n_items[2] = 0;
+        // more than the workspace holds cannot be for valid offsets
+        const bool fits = s_base[1] <= A.part_rows && s_base[0] <= A.most_items;
+        A.counts[0] = fits ? (unsigned)s_base[0] : 0;
+        A.counts[1] = fits ? (unsigned)s_base[2] : 0;
+        A.counts[2] = 0;
     }
 }
 
@@ -843,78 +856,107 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
     constexpr int kBlocks = 2 * (kDim * 256 + 512), kSums = kWaves * 16 * (kDim + 4) * 4 + kWaves * 16 * 8;
     __shared__ __align__(16) char lds[kBlocks > kSums ? kBlocks : kSums];
     __shared__ unsigned s_ticket[2];
-    const u64 n = (u64)A.n_items[0] * A.n_heads;
-    const unsigned stacks = A.n_requests + A.n_groups;
+    const u64 n = (u64)A.counts[0] * A.n_heads;
     // Items are taken as workgroups get free.  Which workgroup computes an item
     // changes nothing in its result.  The next one is asked for early.
     u64 it = blockIdx.x;
     for (unsigned turn = 0; it < n; turn ^= 1) {
-        if (threadIdx.x == 0) s_ticket[turn] = gridDim.x + atomicAdd(&A.n_items[2], 1u);
-        const unsigned entry = (unsigned)(it / A.n_heads), head = (unsigned)(it % A.n_heads);
-        // stacks without items share their first item with the next one, which
-        // is the one that the search gives
-        const unsigned si = wave_search(stacks, entry, [&](unsigned i) { return A.item0[i]; });
-        const Stack s = A.stacks[si];
-        const unsigned local = entry - A.item0[si];
-        const unsigned tiles = (unsigned)tiles_of(A, s);
-        if (s.splits != 0 && local < tiles * s.splits) {
-            const unsigned tile = local % tiles, split = local / tiles;
-            const unsigned rows = tile_rows(A, s);
-            if (rows == 16) few_rows<T, kDim, kE4m3, kWide>(A, s, head, tile, split, lds);
-            else if (rows == 64) many_rows<T, kDim, kE4m3, kWide, 1>(A, s, head, tile, split, lds);
-            else many_rows<T, kDim, kE4m3, kWide, 2>(A, s, head, tile, split, lds);
-        } else {
-            __syncthreads();
-        }
+        if (threadIdx.x == 0) s_ticket[turn] = gridDim.x + atomicAdd(&A.counts[2], 1u);
+        const unsigned head = (unsigned)(it % A.n_heads);
+        const uint4 item = A.items[it / A.n_heads];
+        const Stack s = A.stacks[item.x];
+        const unsigned rows = tile_rows(A, s);
+        if (rows == 16) few_rows<T, kDim, kE4m3, kWide>(A, s, head, item.y, item.z, lds);
+        else if (rows == 64) many_rows<T, kDim, kE4m3, kWide, 1>(A, s, head, item.y, item.z, lds);
+        else many_rows<T, kDim, kE4m3, kWide, 2>(A, s, head, item.y, item.z, lds);
         it = s_ticket[turn];
     }
 }
 
-// Joins the parts of rows that several items share: a wave takes a row, head
-// after head, kDim / 64 columns a lane.
+// Joins the parts of rows that several items share.  A workgroup takes a row and query
+// head at a time: all lanes read the parts' references and sums, then each wave adds up
+// every fourth part, kDim / 64 columns a lane, and the four meet in LDS.  With the parts
+// one after the other in one wave, 128 parts of a long row took 81 us.
 template <class T, int kDim>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
     constexpr int kCols = kDim / 64;
-    const unsigned lane = threadIdx.x % 64;
+    __shared__ float s_w[256], s_top[4], s_sum[4], s_x[3][kDim];
+    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned heads = A.n_heads * A.per;
-    const u64 n = (u64)A.n_rows * heads;
-    u64 w = (u64)blockIdx.x * 4 + threadIdx.x / 64;
-    if (w >= n || !A.n_items[1]) return;
-    const unsigned t = (unsigned)(w / heads), qh = (unsigned)(w % heads);
-    const unsigned r = wave_search(A.n_requests, t, [&](unsigned i) { return A.row_off[i]; });
-    const Stack own = A.stacks[r];
-    if (t < own.row0 || t - own.row0 >= own.rows) return;
-    if (own.part == ~0ull && own.pool == kNone) return;     // written straight out
-    const unsigned head = qh / A.per, g = qh - head * A.per;
-    float top = -INFINITY, sum = 0.f, x[kCols];
-#pragma unroll
-    for (int c = 0; c < kCols; ++c) x[c] = 0.f;
-    for (int which = 0; which < 2; ++which) {
-        const Stack& s = which ? A.stacks[own.pool == kNone ? r : own.pool] : own;
+    const u64 n = (u64)A.counts[1] * heads;
+    for (u64 w = blockIdx.x; w < n; w += gridDim.x) {
+        const unsigned j = (unsigned)(w / heads), qh = (unsigned)(w % heads);
+        const unsigned r = wave_search(A.n_requests, j, [&](unsigned i) { return A.join0[i]; });
+        const Stack own = A.stacks[r];
+        const unsigned t = own.row0 + (j - A.join0[r]);
+        const unsigned head = qh / A.per, g = qh - head * A.per;
+        const Stack pool = A.stacks[own.pool == kNone ? r : own.pool];
+        const u64 own_total = (u64)own.rows * A.per, pool_total = (u64)pool.rows * A.per;
+        const u64 own_first = own.part + (u64)head * own.splits * own_total + (u64)(t - own.row0) * A.per + g;
+        const u64 pool_first = pool.part + (u64)head * pool.splits * pool_total + (u64)(t - pool.row0) * A.per + g;
         // offsets that break the rules can put a request outside its group's rows
-        if (which && (own.pool == kNone || t < s.row0 || t - s.row0 >= s.rows)) break;
-        const u64 total = (u64)s.rows * A.per;
-        const u64 first = s.part + (u64)head * s.splits * total + (u64)(t - s.row0) * A.per + g;
-        for (unsigned i = 0; i < s.splits; ++i) {
-            const float2 ml = A.part_ml[first + i * total];
-            const float best = fmaxf(top, ml.x), ref = best == -INFINITY ? 0.f : best;
-            const float a = exp2f(top - ref), b = exp2f(ml.x - ref);
+        const bool in_pool = own.pool != kNone && t >= pool.row0 && t - pool.row0 < pool.rows;
+        const unsigned parts = own.splits + (in_pool ? pool.splits : 0);
+        auto part = [&](unsigned i) {
+            return i < own.splits ? own_first + i * own_total : pool_first + (i - own.splits) * pool_total;
+        };
+        float top = -INFINITY, sum = 0.f, x[kCols];
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) x[c] = 0.f;
+        for (unsigned i0 = 0; i0 < parts; i0 += 256) {
+            const unsigned i = i0 + threadIdx.x;
+            const float2 ml = i < parts ? A.part_ml[part(i)] : float2{-INFINITY, 0.f};
+            float best = ml.x;
+#pragma unroll
+            for (int m = 32; m; m >>= 1) best = fmaxf(best, __shfl_xor(best, m));
+            if (lane == 0) s_top[wave] = best;
+            __syncthreads();
+            best = fmaxf(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), top);
+            const float ref = best == -INFINITY ? 0.f : best, shrink = exp2f(top - ref);
+            const float weight = exp2f(ml.x - ref);
+            s_w[threadIdx.x] = weight;
+            float part_sum = ml.y * weight;
+#pragma unroll
+            for (int m = 32; m; m >>= 1) part_sum += __shfl_xor(part_sum, m);
+            if (lane == 0) s_sum[wave] = part_sum;
+            __syncthreads();
+            sum = sum * shrink + ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
             top = best;
-            sum = sum * a + ml.y * b;
-            const float* p = &A.part_o[(first + i * total) * kDim + lane * kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) x[c] *= shrink;
+            const unsigned k = min(256u, parts - i0);
+#pragma unroll 8
+            for (unsigned i = wave; i < k; i += 4) {
+                const float* from = &A.part_o[part(i0 + i) * kDim + lane * kCols];
+                const float f = s_w[i];
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) x[c] += lane * kCols < A.dim ? from[c] * f : 0.f;
+            }
+            __syncthreads();
+        }
+        if (wave) {
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) s_x[wave - 1][lane * kCols + c] = x[c];
+        }
+        __syncthreads();
+        if (wave == 0) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
             for (int c = 0; c < kCols; ++c)
-                x[c] = x[c] * a + (lane * kCols + c < A.dim ? p[c] * b : 0.f);
-        }
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    char* to = A.out + (u64)t * A.out_row + (u64)qh * A.out_head;
+                x[c] = (((x[c] + s_x[0][lane * kCols + c]) + s_x[1][lane * kCols + c]) + s_x[2][lane * kCols + c]) * inv;
+            unsigned short* to = reinterpret_cast<unsigned short*>(A.out + (u64)t * A.out_row + (u64)qh * A.out_head) + lane * kCols;
+            if (lane * kCols < A.dim) {
+                if constexpr (kCols == 1) {
+                    *to = (unsigned short)T::pack(x[0], 0.f);
+                } else {
 #pragma unroll
-    for (int c = 0; c < kCols; ++c)
-        if (lane * kCols + c < A.dim)
-            reinterpret_cast<unsigned short*>(to)[lane * kCols + c] =
-                (unsigned short)T::pack(x[c] * inv, 0.f);
-    if (A.lse && lane == 0) A.lse[(u64)t * heads + qh] = (top + log2f(sum)) * 0.6931471805599453f;
+                    for (int c = 0; c < kCols; c += 2) reinterpret_cast<unsigned*>(to)[c / 2] = T::pack(x[c], x[c + 1]);
+                }
+            }
+            if (A.lse && lane == 0) A.lse[(u64)t * heads + qh] = (top + log2f(sum)) * 0.6931471805599453f;
+        }
+        __syncthreads();
+    }
 }
 
 unsigned padded(unsigned dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
@@ -927,14 +969,19 @@ u64 part_rows(u64 n_rows, u64 n_q_heads) {
     return 2 * n_rows * n_q_heads + (u64)kTarget * kMostRows;
 }
 
+// Items per head at most: a tile of every 16 rows and every stack's last one, once for
+// own tokens and once for prefixes, and the splits.
+u64 most_items(u64 n_rows, u64 n_stacks, u64 per) { return 2 * (n_rows * per / 16) + n_stacks + kTarget; }
+
 struct Layout {
-    u64 item0, stacks, ml, o, bytes;
+    u64 items, join0, stacks, ml, o, bytes;
 };
-Layout layout_of(u64 n_rows, u64 n_requests, u64 n_groups, u64 n_q_heads, unsigned dim) {
+Layout layout_of(u64 n_rows, u64 n_requests, u64 n_groups, u64 n_heads, u64 per, unsigned dim) {
     Layout l;
-    const u64 n = n_requests + n_groups, rows = part_rows(n_rows, n_q_heads);
-    l.item0 = 256;
-    l.stacks = up(l.item0 + 4 * (n + 1));
+    const u64 n = n_requests + n_groups, rows = part_rows(n_rows, n_heads * per);
+    l.items = 256;
+    l.join0 = up(l.items + sizeof(uint4) * most_items(n_rows, n, per));
+    l.stacks = up(l.join0 + 4 * n_requests);
     l.ml = up(l.stacks + sizeof(Stack) * n);
     l.o = up(l.ml + 8 * rows);
     l.bytes = l.o + 4 * rows * padded(dim);
@@ -947,8 +994,9 @@ void attend_launch(const AttendArgs& A, unsigned cus, hipStream_t st) {
     const dim3 grid(cus * (kDim > 128 ? 1 : 2)), block(kWaves * 64);
     if (A.shift >= 4) hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, true>), grid, block, 0, st, A);
     else hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, false>), grid, block, 0, st, A);
-    const u64 waves = (u64)A.n_rows * A.n_heads * A.per;
-    hipLaunchKernelGGL((k_attend_join<T, kDim>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, A);
+    const u64 rows = (u64)A.n_rows * A.n_heads * A.per;
+    hipLaunchKernelGGL((k_attend_join<T, kDim>), dim3((unsigned)std::min<u64>(rows, 8 * cus)), dim3(256), 0,
+                       st, A);
 }
 
 template <class T, bool kE4m3>
@@ -983,7 +1031,8 @@ uint64_t ss_prefix_attention_workspace(const ss_kv_cache* cache, const ss_batch*
                                        uint32_t n_q_heads) {
     if (!cache || attend_args(cache, batch, cache->type == SS_F16 ? SS_F16 : SS_BF16, n_q_heads) != SS_OK)
         return 0;
-    return layout_of(batch->n_rows, batch->n_requests, batch->n_groups, n_q_heads, cache->head_dim).bytes;
+    return layout_of(batch->n_rows, batch->n_requests, batch->n_groups, cache->n_heads,
+                     n_q_heads / cache->n_heads, cache->head_dim).bytes;
 }
 
 ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, const void* q,
@@ -1000,7 +1049,8 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     if ((s = rows_args("q", q, rows, n_q_heads, dim, q_row_stride, q_head_stride, false)) != SS_OK ||
         (s = rows_args("out", out, rows, n_q_heads, dim, out_row_stride, out_head_stride, true)) != SS_OK)
         return s;
-    const Layout l = layout_of(rows, batch->n_requests, batch->n_groups, n_q_heads, dim);
+    const Layout l = layout_of(rows, batch->n_requests, batch->n_groups, cache->n_heads,
+                               n_q_heads / cache->n_heads, dim);
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))
         return set_err(SS_ERR_ARG, "workspace must be a 16-byte aligned pointer");
     if (workspace_bytes < l.bytes)
@@ -1057,8 +1107,10 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     A.q_keep = scale == 0.f ? 0u : ~0u;
     A.q_flip = scale < 0.f ? 0x80008000u : 0u;
     char* ws = static_cast<char*>(workspace);
-    A.n_items = reinterpret_cast<unsigned*>(ws);
-    A.item0 = reinterpret_cast<unsigned*>(ws + l.item0);
+    A.counts = reinterpret_cast<unsigned*>(ws);
+    A.items = reinterpret_cast<uint4*>(ws + l.items);
+    A.join0 = reinterpret_cast<unsigned*>(ws + l.join0);
+    A.most_items = most_items(rows, batch->n_requests + batch->n_groups, n_q_heads / cache->n_heads);
     A.stacks = reinterpret_cast<Stack*>(ws + l.stacks);
     A.part_ml = reinterpret_cast<float2*>(ws + l.ml);
     A.part_o = reinterpret_cast<float*>(ws + l.o);

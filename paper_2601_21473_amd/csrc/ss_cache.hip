@@ -28,6 +28,7 @@ struct CacheArgs {
     unsigned n_heads, dim;
     unsigned shift;                 // page_tokens = 1 << shift
     unsigned rows_per_block;        // 1, 2, 4, 8 or 16
+    unsigned per_row_inv;           // 2^32 / (2 n_heads), rounded up
 };
 
 constexpr int kCacheThreads = 256;
@@ -58,16 +59,19 @@ __device__ inline int place_of(const CacheArgs& A, unsigned t, unsigned sub, uns
 }
 
 // One workgroup moves rows_per_block rows of keys and values.  kWrite: rows to
-// pages.  kLanes lanes hold a head's row, 8 values each (dim <= 8 kLanes).
+// pages.  kLanes lanes hold a head's row, 8 values each (dim <= 8 kLanes); four rows'
+// reads are in flight at a time.
 template <class T, bool kE4m3, bool kWrite, int kLanes>
 __global__ __launch_bounds__(kCacheThreads) void k_cache(CacheArgs A) {
+    constexpr unsigned kAtOnce = 4, kGroups = kCacheThreads / kLanes;
     __shared__ int s_unit[16];
     __shared__ unsigned s_slot[16];
     const unsigned row0 = blockIdx.x * A.rows_per_block;
     {
         const unsigned i = threadIdx.x / 16, sub = threadIdx.x % 16;
         unsigned slot = 0;
-        const int u = place_of(A, row0 + i, sub, &slot);
+        int u = -2;
+        if (i < A.rows_per_block) u = place_of(A, row0 + i, sub, &slot);
         if (sub == 0) {
             s_unit[i] = u;
             s_slot[i] = slot;
@@ -75,42 +79,63 @@ __global__ __launch_bounds__(kCacheThreads) void k_cache(CacheArgs A) {
     }
     __syncthreads();
     const unsigned per_row = 2 * A.n_heads;                 // head rows of keys and values
+    const unsigned all = per_row * A.rows_per_block;        // at most 2^15
     const unsigned d0 = (threadIdx.x % kLanes) * 8;
     const bool in = d0 < A.dim;
-    for (unsigned g = threadIdx.x / kLanes; g < per_row * A.rows_per_block;
-         g += kCacheThreads / kLanes) {
-        const unsigned i = g / per_row, wh = g % per_row;
-        const int unit = s_unit[i];
-        if (unit < (kWrite ? 0 : -1)) continue;
-        const unsigned what = wh >= A.n_heads, h = wh - (what ? A.n_heads : 0);
-        char* row = A.rows[what] + (u64)(row0 + i) * A.row_stride + (u64)h * A.head_stride + d0 * 2;
-        const unsigned slot = s_slot[i];
-        char* base = A.plane[what] + (u64)(unit < 0 ? 0 : unit) * A.unit_bytes[what];
-        char* cell = base + (u64)slot * A.token_bytes + (u64)h * A.head_bytes + d0 * (kE4m3 ? 1 : 2);
-        float* scale_at = reinterpret_cast<float*>(base + A.scale_off) + ((u64)h << A.shift) + slot;
-        if constexpr (kWrite) {
-            u32x4 w = {0, 0, 0, 0};
-            if (in) w = *reinterpret_cast<const u32x4*>(row);
-            if constexpr (!kE4m3) {
-                if (in) *reinterpret_cast<u32x4*>(cell) = w;
+    for (unsigned g0 = threadIdx.x / kLanes; g0 < all; g0 += kGroups * kAtOnce) {
+        u32x4 w[kAtOnce];
+        float scale[kAtOnce];
+        char* row[kAtOnce];
+        char* cell[kAtOnce];
+        float* scale_at[kAtOnce];
+        int unit[kAtOnce];
+#pragma unroll
+        for (unsigned a = 0; a < kAtOnce; ++a) {
+            const unsigned g = g0 + a * kGroups;
+            // g / per_row: exact for g below 2^16 (g times the factor's excess is below 2^32)
+            const unsigned i = g < all ? __umulhi(g, A.per_row_inv) : 0, wh = g - i * per_row;
+            unit[a] = g < all ? s_unit[i] : -2;
+            const unsigned slot = s_slot[i];
+            const unsigned what = wh >= A.n_heads, h = wh - (what ? A.n_heads : 0);
+            row[a] = A.rows[what] + (u64)(row0 + i) * A.row_stride + (u64)h * A.head_stride + d0 * 2;
+            char* base = A.plane[what] + (u64)(unit[a] < 0 ? 0 : unit[a]) * A.unit_bytes[what];
+            cell[a] = base + (u64)slot * A.token_bytes + (u64)h * A.head_bytes + d0 * (kE4m3 ? 1 : 2);
+            scale_at[a] = reinterpret_cast<float*>(base + A.scale_off) + ((u64)h << A.shift) + slot;
+            w[a] = u32x4{0, 0, 0, 0};
+            if (unit[a] < 0 || !in) continue;
+            if constexpr (kWrite) {
+                w[a] = *reinterpret_cast<const u32x4*>(row[a]);
+            } else if constexpr (!kE4m3) {
+                w[a] = *reinterpret_cast<const u32x4*>(cell[a]);
             } else {
+                const u32x2 c = *reinterpret_cast<const u32x2*>(cell[a]);
+                w[a] = u32x4{c[0], c[1], 0, 0};
+                scale[a] = *scale_at[a];
+            }
+        }
+#pragma unroll
+        for (unsigned a = 0; a < kAtOnce; ++a) {
+            if (unit[a] < (kWrite ? 0 : -1)) continue;
+            if constexpr (!kE4m3) {
+                if (in) *reinterpret_cast<u32x4*>(kWrite ? cell[a] : row[a]) = w[a];
+            } else if constexpr (kWrite) {
                 float x[8], top = 0.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    x[2 * j] = T::lo(w[j]);
-                    x[2 * j + 1] = T::hi(w[j]);
+                    x[2 * j] = T::lo(w[a][j]);
+                    x[2 * j + 1] = T::hi(w[a][j]);
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float a = fabsf(x[j]);
-                    top = a < INFINITY && a > top ? a : top;        // NaN is neither
+                    const float y = fabsf(x[j]);
+                    top = y < INFINITY && y > top ? y : top;        // NaN is neither
                 }
 #pragma unroll
                 for (int m = kLanes / 2; m; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-                const float scale = fmaxf(top / 448.f, 0x1p-126f);
+                const float s = fmaxf(top / 448.f, 0x1p-126f);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float q = x[j] / scale;
+                    const float q = x[j] / s;
                     x[j] = q > 448.f ? 448.f : q < -448.f ? -448.f : q;     // NaN stays
                 }
                 int lo = 0, hi = 0;
@@ -118,27 +143,21 @@ __global__ __launch_bounds__(kCacheThreads) void k_cache(CacheArgs A) {
                 lo = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], lo, true);
                 hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[4], x[5], hi, false);
                 hi = __builtin_amdgcn_cvt_pk_fp8_f32(x[6], x[7], hi, true);
-                if (in) *reinterpret_cast<u32x2*>(cell) = u32x2{(unsigned)lo, (unsigned)hi};
-                if (d0 == 0) *scale_at = scale;
-            }
-        } else {
-            u32x4 w = {0, 0, 0, 0};
-            if (unit >= 0 && in) {
-                if constexpr (!kE4m3) {
-                    w = *reinterpret_cast<const u32x4*>(cell);
-                } else {
-                    const u32x2 c = *reinterpret_cast<const u32x2*>(cell);
-                    const float s = *scale_at;
+                if (in) *reinterpret_cast<u32x2*>(cell[a]) = u32x2{(unsigned)lo, (unsigned)hi};
+                if (d0 == 0) *scale_at[a] = s;
+            } else {
+                u32x4 y = {0, 0, 0, 0};
+                if (unit[a] >= 0) {
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[j], false);
-                        const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[j], true);
-                        w[2 * j] = T::pack(a[0] * s, a[1] * s);
-                        w[2 * j + 1] = T::pack(b[0] * s, b[1] * s);
+                        const auto p = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[a][j], false);
+                        const auto q = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[a][j], true);
+                        y[2 * j] = T::pack(p[0] * scale[a], p[1] * scale[a]);
+                        y[2 * j + 1] = T::pack(q[0] * scale[a], q[1] * scale[a]);
                     }
                 }
+                if (in) *reinterpret_cast<u32x4*>(row[a]) = y;
             }
-            if (in) *reinterpret_cast<u32x4*>(row) = w;
         }
     }
 }
@@ -190,6 +209,7 @@ ss_status cache_call(const ss_kv_cache* c, const ss_batch* b, const void* k, con
     A.n_requests = b->n_requests;
     A.n_heads = c->n_heads;
     A.dim = c->head_dim;
+    A.per_row_inv = (unsigned)((1ull << 32) / (2 * c->n_heads) + 1);
     A.shift = (unsigned)__builtin_ctz(c->page_tokens);
     // the search for the rows' requests costs a block as much for one row as for
     // 16, so blocks take more rows once there are 1,024 blocks
