@@ -529,7 +529,9 @@ ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, v
  * of a request see leaves its earlier rows of the same call unspecified.
  *   q, out     [n_rows][n_q_heads][head_dim] SS_BF16 or SS_F16 (`type`; the
  *              cache's unless that is SS_E4M3), strides in elements (multiples
- *              of 8), 16-byte aligned; out must not overlap q;
+ *              of 8), 16-byte aligned; out must not overlap q; n_rows * n_q_heads
+ *              must be below 2^30;
+ *              n_rows * n_q_heads must be below 2^30;
  *   lse        [n_rows][n_q_heads] floats, or NULL;
  *   scale      finite (1 / sqrt(head_dim) as a rule);
  *   workspace  ss_prefix_attention_workspace(...) bytes (a bound over all

@@ -20,7 +20,7 @@ namespace {
 
 constexpr unsigned kTile = 16;          // rows of a tile of k_adapter_in
 constexpr int kThreads = 256;
-constexpr unsigned kOutCols = 512;      // columns of out per workgroup, 128 a wave
+constexpr unsigned kOutCols = 512;      // columns of out per round of a workgroup, 128 a wave
 
 struct AdapterArgs {
     Table tab;
@@ -38,6 +38,7 @@ struct AdapterArgs {
     unsigned n_rows, n_requests;
     float* low;                         // [pieces][n_rows][rank]: parts of A x
     unsigned pieces, piece;             // pieces of n_in, and elements of one
+    unsigned cols;                      // columns of out per workgroup
 };
 
 // Tile i of the batch: request r's tiles begin at row_off[r] / kTile + r, which leaves
@@ -117,8 +118,8 @@ __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
     }
 }
 
-// A workgroup per tile of up to 16 kSub rows and kOutCols columns; a wave takes 128 of
-// them.  A x enters as two 16-bit parts, the rounded value and what the rounding left,
+// A workgroup per tile of up to 16 kSub rows and A.cols columns; a wave takes 128 of each
+// 512 of them.  A x enters as two 16-bit parts, the rounded value and what the rounding left,
 // so that its 32 bits count for 16 (bf16) or 22 (fp16) of them; for fp16 each row is
 // first divided by a power of two near its largest value, as sums can pass that type's
 // range.  Up to rank 16 both parts fit next to each other into one product's 32 summed
@@ -127,43 +128,47 @@ __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
 // columns next to each other of four rows and moves them in 16 bytes, with nothing
 // exchanged.  HBM bounds it: base and B are asked for before the wait for A x.
 template <class T, int kSub, bool kPacked>
-__global__ __launch_bounds__(kThreads, kSub == 1 ? 4 : 2) void k_adapter_out(AdapterArgs A) {
+__global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(AdapterArgs A) {
     constexpr unsigned kRows = 16 * kSub, kPitch = kPacked ? 40 : 2 * 128 + 8;
     __shared__ __align__(16) unsigned short s_h[kRows][kPitch];     // two parts, zeros behind
     __shared__ float s_scale[kRows];
     unsigned r, row0;
-    const unsigned parts = (A.n_out + kOutCols - 1) / kOutCols;
+    const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
     const unsigned rows = tile_of<kRows>(A, blockIdx.x / parts, &r, &row0);
     if (!rows) return;
     const int unit = adapter_of(A, r);
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned col = lane % 16, quad = lane / 16;
-    const unsigned n = blockIdx.x % parts * kOutCols + wave * 128 + 8 * col;    // first of eight
-    const bool in = n < A.n_out;
-    const u64 out_at = (u64)n * 2;
-    // the first 16 rows' share of base, and B for the first 32 ranks
-    u32x4 base[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const unsigned t = 4 * quad + i;
-        base[i] = u32x4{0, 0, 0, 0};
-        if (in && t < rows)
-            base[i] = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + out_at);
-    }
+    const unsigned n0 = blockIdx.x % parts * A.cols + wave * 128;       // the wave's, the same
+    const unsigned n1 = min(A.n_out, blockIdx.x % parts * A.cols + A.cols);     // for all lanes
     const unsigned rank8 = A.rank / 8;
-    const char* const bm = A.b + (u64)(unit < 0 ? 0 : unit) * A.b_unit + (u64)(in ? n : 0) * A.rank * 2;
-    // eight ranks of the lane's column j in step k: packed, ranks and parts go round
-    auto load_b = [&](unsigned k, u32x4* b) {
+    const char* const bm = A.b + (u64)(unit < 0 ? 0 : unit) * A.b_unit;
+    auto load_base = [&](unsigned n, u32x4 (*base)[4]) {
+#pragma unroll
+        for (int s = 0; s < kSub; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned t = 16 * s + 4 * quad + i;
+                base[s][i] = u32x4{0, 0, 0, 0};
+                if (n < n1 && t < rows)
+                    base[s][i] = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + (u64)n * 2);
+            }
+    };
+    // eight ranks of columns n .. n + 7 in step k: packed, ranks and parts go round
+    auto load_b = [&](unsigned n, unsigned k, u32x4* b) {
         const unsigned c = 4 * k + quad, from = kPacked && c >= rank8 ? c - rank8 : c;
+        const bool there = n < n1 && from < rank8;
+        const unsigned at = there ? (n * rank8 + from) * 16 : 0;         // below 2^31
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            b[j] = u32x4{0, 0, 0, 0};
-            if (from < rank8) b[j] = *reinterpret_cast<const u32x4*>(bm + ((u64)j * rank8 + from) * 16);
+            b[j] = *reinterpret_cast<const u32x4*>(bm + (there ? at + j * A.rank * 2 : 0u));
+            if (!there) b[j] = u32x4{0, 0, 0, 0};
         }
     };
-    u32x4 bf[8];
-    if (unit >= 0) load_b(0, bf);
+    u32x4 base[kSub][4], bf[8];
+    load_base(n0 + 8 * col, base);
+    if (unit >= 0) load_b(n0 + 8 * col, 0, bf);
     if (unit >= 0) {
         // 16 lanes a row: eight ranks each
         for (unsigned i0 = 0; i0 < kRows; i0 += 16) {
@@ -220,66 +225,65 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 4 : 2) void k_adapter_out(Ada
         }
         __syncthreads();
     }
-    f32x4 acc[kSub][8];
+#pragma unroll 1
+    for (unsigned nw = n0; nw < n1; nw += kOutCols) {
+        const unsigned n = nw + 8 * col;                // the lane's first of eight
+        f32x4 acc[kSub][8];
 #pragma unroll
-    for (int t = 0; t < kSub; ++t)
+        for (int t = 0; t < kSub; ++t)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[t][j] = f32x4{0, 0, 0, 0};
-    if (unit >= 0) {
-        const unsigned steps = kPacked ? 1 : (A.rank + 31) / 32;
-        for (unsigned k = 0; k < steps; ++k) {
-            u32x4 next[8];
-            if (!kPacked && k + 1 < steps) load_b(k + 1, next);
+            for (int j = 0; j < 8; ++j) acc[t][j] = f32x4{0, 0, 0, 0};
+        if (unit >= 0) {
+            const unsigned steps = kPacked ? 1 : (A.rank + 31) / 32;
+#pragma unroll 1
+            for (unsigned k = 0; k < steps; ++k) {
 #pragma unroll
-            for (int t = 0; t < kSub; ++t) {
-                const unsigned short* h = &s_h[16 * t + col][32 * k + 8 * quad];
-                const u32x4 high = *reinterpret_cast<const u32x4*>(h);
+                for (int t = 0; t < kSub; ++t) {
+                    const unsigned short* h = &s_h[16 * t + col][32 * k + 8 * quad];
+                    const u32x4 high = *reinterpret_cast<const u32x4*>(h);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(high, bf[j], acc[t][j]);
-                if constexpr (!kPacked) {
-                    const u32x4 rest = *reinterpret_cast<const u32x4*>(h + 128);
+                    for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(high, bf[j], acc[t][j]);
+                    if constexpr (!kPacked) {
+                        const u32x4 rest = *reinterpret_cast<const u32x4*>(h + 128);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(rest, bf[j], acc[t][j]);
+                        for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(rest, bf[j], acc[t][j]);
+                    }
                 }
-            }
-            if (!kPacked && k + 1 < steps) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) bf[j] = next[j];
+                if (k + 1 < steps) load_b(n, k + 1, bf);
+                else load_b(n + kOutCols, 0, bf);
             }
         }
-    }
 #pragma unroll
-    for (int s = 0; s < kSub; ++s) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned t = 16 * s + 4 * quad + i;
-            if (!in || t >= rows) continue;
-            u32x4 w = base[i];
-            if (unit >= 0) {
-                const float f = s_scale[t];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    w[j] = T::pack(T::lo(w[j]) + f * acc[s][2 * j][i], T::hi(w[j]) + f * acc[s][2 * j + 1][i]);
-            }
-            *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + t) * A.out_row + out_at) = w;
-        }
-        if (s + 1 < kSub) {
+        for (int s = 0; s < kSub; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const unsigned t = 16 * (s + 1) + 4 * quad + i;
-                if (in && t < rows)
-                    base[i] = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + out_at);
+                const unsigned t = 16 * s + 4 * quad + i;
+                if (n >= n1 || t >= rows) continue;
+                u32x4 w = base[s][i];
+                if (unit >= 0) {
+                    const float f = s_scale[t];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = T::pack(T::lo(w[j]) + f * acc[s][2 * j][i], T::hi(w[j]) + f * acc[s][2 * j + 1][i]);
+                }
+                *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + t) * A.out_row + (u64)n * 2) = w;
             }
-        }
+        load_base(n + kOutCols, base);
     }
 }
 
 template <class T, int kSub>
 void out_launch(const AdapterArgs& A, hipStream_t st) {
     const unsigned tiles = A.n_rows / (16 * kSub) + A.n_requests;
-    const dim3 grid((A.n_out + kOutCols - 1) / kOutCols * tiles), block(kThreads);
-    if (A.rank <= 16) hipLaunchKernelGGL((k_adapter_out<T, kSub, true>), grid, block, 0, st, A);
-    else hipLaunchKernelGGL((k_adapter_out<T, kSub, false>), grid, block, 0, st, A);
+    // a workgroup reads its way to the adapter before it streams, so it takes several
+    // 512 columns once there are 1,024 workgroups
+    const unsigned pieces = (A.n_out + kOutCols - 1) / kOutCols;
+    const unsigned each = std::max(1u, std::min<unsigned>(pieces, (unsigned)((u64)pieces * tiles / 1024)));
+    AdapterArgs B = A;
+    B.cols = kOutCols * each;
+    const dim3 grid((pieces + each - 1) / each * tiles), block(kThreads);
+    if (A.rank <= 16) hipLaunchKernelGGL((k_adapter_out<T, kSub, true>), grid, block, 0, st, B);
+    else hipLaunchKernelGGL((k_adapter_out<T, kSub, false>), grid, block, 0, st, B);
 }
 
 template <class T>
@@ -293,8 +297,8 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
         case 4: hipLaunchKernelGGL((k_adapter_in<T, 4>), in, block, 0, st, A); break;
         default: hipLaunchKernelGGL((k_adapter_in<T, 8>), in, block, 0, st, A); break;
     }
-    // tiles of 64 rows where requests fill them: B is read a quarter as often
-    if (A.n_rows >= 32ull * A.n_requests) out_launch<T, 4>(A, st);
+    // tiles of 32 rows where requests fill them: B is read half as often
+    if (A.n_rows >= 24ull * A.n_requests) out_launch<T, 2>(A, st);
     else out_launch<T, 1>(A, st);
 }
 
@@ -324,6 +328,8 @@ ss_status adapter_args(const ss_adapters* a) {
     if (a->a_unit_bytes % 16 || a->b_unit_bytes % 16 || a->a_unit_bytes >= (1ull << 31) ||
         a->b_unit_bytes >= (1ull << 31))
         return set_err(SS_ERR_ARG, "adapter byte distances must be multiples of 16 below 2^31");
+    if (2ull * a->rank * std::max(a->n_in, a->n_out) >= (1ull << 31))
+        return set_err(SS_ERR_ARG, "a matrix is too large (2^31 bytes)");
     if (a->capacity_units > 1 && (a->a_unit_bytes < 2ull * a->rank * a->n_in ||
                                   a->b_unit_bytes < 2ull * a->rank * a->n_out))
         return set_err(SS_ERR_ARG, "a matrix does not fit into a unit's chunk");

@@ -31,11 +31,32 @@ struct Stack {
     unsigned keys[2];   // tokens with a page
     unsigned row0, rows;
     int see;            // row i of the stack sees own tokens 0 .. see + i
-    unsigned chunk;     // key blocks of an item
     unsigned splits;    // items per tile and head
-    unsigned pool;      // a request's stack: the stack of its group's prefix, or kNone
+    unsigned pool;      // a request's stack: its group, if that has a stack of its own, or kNone
+    unsigned pad;
 };
 static_assert(sizeof(Stack) == 56, "three words and eight halves");
+
+// An item, the same for every head.
+struct Item {
+    u64 first[2];
+    u64 part;
+    unsigned keys[2];
+    unsigned row0, rows;
+    int see;
+    unsigned splits;
+    unsigned tile_rows, tile, split, chunk;     // key blocks [split chunk, (split + 1) chunk)
+};
+static_assert(sizeof(Item) == 64, "four 16-byte words");
+
+// A row whose parts are joined: its own tokens' and its prefix's.
+struct JoinRow {
+    u64 first[2];       // the part of head 0, query head 0, split 0
+    unsigned total[2];  // rows of the stack: the distance between splits
+    unsigned splits[2];
+    unsigned row, pad[3];
+};
+static_assert(sizeof(JoinRow) == 48, "three 16-byte words");
 
 struct AttendArgs {
     Table tab;
@@ -59,16 +80,16 @@ struct AttendArgs {
     unsigned q_keep, q_flip;                    // queries' bits that count, and that turn
     // workspace
     unsigned* counts;                           // items per head, rows to join, items taken
-    uint4* items;                               // [most_items] stack, tile, split
-    unsigned* join0;                            // [n_requests] rows to join before each request's
-    Stack* stacks;                              // [n_requests + n_groups]
+    Item* items;                                // [most_items]
+    JoinRow* joins;                             // [n_rows]
+    Stack* stacks;                              // [n_groups] of the prefixes
     u64 most_items;
     float* part_o;                              // [part_rows][padded dim]
     float2* part_ml;                            // [part_rows] maximum (log2), sum
     u64 part_rows;
 };
 
-constexpr int kPlanThreads = 1024;
+constexpr unsigned kPlanThreads = 512;
 
 __device__ unsigned tokens_with_page(const AttendArgs& A, unsigned agent, unsigned len, u64* first) {
     const u64 most = (u64)A.tab.row(agent, first) << A.shift;
@@ -111,7 +132,7 @@ __device__ Stack prefix_stack(const AttendArgs& A, unsigned g) {
     return t;
 }
 
-// The stack of request s's own tokens (and of its prefix, where that has none).
+// The stack of request s's own tokens, without its prefix.
 __device__ Stack request_stack(const AttendArgs& A, unsigned s) {
     Stack t{};
     t.part = ~0ull;
@@ -125,134 +146,199 @@ __device__ Stack request_stack(const AttendArgs& A, unsigned s) {
     u64 first;
     t.keys[1] = tokens_with_page(A, agent, len, &first);
     t.first[1] = first;
+    return t;
+}
+
+// Adds request s's prefix, if its group has one: as keys of its own or as a pool.
+__device__ void add_prefix(const AttendArgs& A, unsigned s, Stack& t) {
     unsigned lo = 0, hi = A.n_groups;           // the largest g with group_off[g] <= s
     while (hi - lo > 1) {
         const unsigned mid = (lo + hi) / 2;
         if (A.group_off[mid] <= s) lo = mid;
         else hi = mid;
     }
-    if (hi > lo && A.group_off[lo] <= s && s < A.group_off[lo + 1]) {
-        const Stack& p = A.stacks[A.n_requests + lo];
-        if (p.rows) {
-            t.pool = A.n_requests + lo;
-        } else {
-            t.keys[0] = p.keys[0];
-            t.first[0] = p.first[0];
-        }
+    if (hi <= lo || A.group_off[lo] > s || s >= A.group_off[lo + 1]) return;
+    const Stack& p = A.stacks[lo];
+    if (p.rows) {
+        t.pool = lo;
+    } else {
+        t.keys[0] = p.keys[0];
+        t.first[0] = p.first[0];
     }
-    return t;
 }
 
-// One workgroup: the stacks, how they are split, the list of items and where each
-// stack's parts begin.  Keys are cut into pieces of about 1/kTarget of the call's
-// work.  A few reads one after the other bound it, so groups come first and requests
-// look theirs up.
+// What the planning workgroup carries from one thousand stacks to the next.
+struct PlanState {
+    Stack stack[kPlanThreads];
+    unsigned at[2][kPlanThreads + 1];           // first item, first row to join, of each stack
+    unsigned sum[kPlanThreads / 64][3];
+    unsigned base[3];                           // items, rows to join, parts per head so far
+};
+
+// Lists the items and the rows to join of up to kPlanThreads stacks, thread by thread.
+__device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned group, unsigned chunk,
+                            PlanState& S) {
+    const unsigned tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const unsigned blocks = blocks_of(t);
+    t.splits = blocks / chunk + (blocks % chunk != 0);
+    if (own && t.pool == kNone && t.splits == 0) t.splits = 1;          // writes zeros
+    if (!t.rows) t.splits = 0;
+    const bool joined = own && (t.splits > 1 || t.pool != kNone);
+    const unsigned v[3] = {tiles_of(A, t) * t.splits, joined ? t.rows : 0,
+                           joined || !own ? t.rows * A.per * t.splits : 0};
+    // exclusive sums over the workgroup
+    unsigned a[3] = {v[0], v[1], v[2]};
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+            const unsigned x = __shfl_up(a[k], m);
+            if (lane >= (unsigned)m) a[k] += x;
+        }
+    if (lane == 63) {
+#pragma unroll
+        for (int k = 0; k < 3; ++k) S.sum[wave][k] = a[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        a[k] -= v[k];
+        for (unsigned w = 0; w < wave; ++w) a[k] += S.sum[w][k];
+    }
+    if (v[2]) t.part = (u64)(S.base[2] + a[2]) * A.n_heads;
+    if (group != kNone) A.stacks[group] = t;
+    S.stack[tid] = t;
+    S.at[0][tid] = a[0];
+    S.at[1][tid] = a[1];
+    if (tid == kPlanThreads - 1) {
+        S.at[0][kPlanThreads] = a[0] + v[0];
+        S.at[1][kPlanThreads] = a[1] + v[1];
+    }
+    __syncthreads();
+    // the stack of an item or row: the last that begins at or before it
+    auto find = [&](int k, unsigned i) {
+        unsigned lo = 0;
+#pragma unroll
+        for (unsigned step = kPlanThreads / 2; step; step /= 2)
+            if (S.at[k][lo + step] <= i) lo += step;
+        return lo;
+    };
+    const unsigned items = S.at[0][kPlanThreads], joins = S.at[1][kPlanThreads];
+    if ((u64)S.base[0] + items <= A.most_items)
+        for (unsigned i = tid; i < items; i += kPlanThreads) {
+            const unsigned f = find(0, i), j = i - S.at[0][f];
+            const Stack& s = S.stack[f];
+            const unsigned tiles = tiles_of(A, s);
+            // tiles next to each other read the same keys
+            A.items[S.base[0] + i] = Item{{s.first[0], s.first[1]}, s.part, {s.keys[0], s.keys[1]},
+                                          s.row0, s.rows, s.see, s.splits, tile_rows(A, s),
+                                          j % tiles, j / tiles, chunk};
+        }
+    if ((u64)S.base[1] + joins <= A.n_rows)
+        for (unsigned i = tid; i < joins; i += kPlanThreads) {
+            const unsigned f = find(1, i);
+            const Stack& s = S.stack[f];
+            JoinRow r{};
+            r.row = s.row0 + (i - S.at[1][f]);
+            r.first[0] = s.part + (u64)(r.row - s.row0) * A.per;
+            r.total[0] = s.rows * A.per;
+            r.splits[0] = s.splits;
+            if (s.pool != kNone) {
+                const Stack& p = A.stacks[s.pool];
+                // offsets that break the rules can put a request outside its group's rows
+                if (r.row >= p.row0 && r.row - p.row0 < p.rows) {
+                    r.first[1] = p.part + (u64)(r.row - p.row0) * A.per;
+                    r.total[1] = p.rows * A.per;
+                    r.splits[1] = p.splits;
+                }
+            }
+            A.joins[S.base[1] + i] = r;
+        }
+    __syncthreads();
+    if (tid == kPlanThreads - 1) {
+        S.base[0] += a[0] + v[0];
+        S.base[1] += a[1] + v[1];
+        S.base[2] += a[2] + v[2];
+    }
+    __syncthreads();
+}
+
+// One workgroup: the stacks, how they are split, and what there is to do.  Keys are cut
+// into pieces of about 1/kTarget of the call's work.  Reads that wait for each other
+// bound it, so a request's own ones are out before its group is looked at, and items and
+// joins carry all that their kernels need.
 __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
-    __shared__ u64 s_sum[kPlanThreads / 64][3];
-    __shared__ u64 s_base[3];
-    const unsigned n = A.n_requests + A.n_groups, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    u64 work = 0, own_rows = 0, pool_rows = 0;
+    __shared__ PlanState S;
+    __shared__ float s_work[kPlanThreads / 64];
+    __shared__ unsigned s_rows[kPlanThreads / 64][2];
+    const unsigned tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    // work in 32-bit floats: it only sets how fine the pieces are
+    float work = 0.f;
+    unsigned own_rows = 0, pool_rows = 0;       // saturating: one of n_rows says enough
+    auto add = [](unsigned a, unsigned b) { return a + b < a ? ~0u : a + b; };
+    Stack mine{};
+    if (tid < A.n_requests) mine = request_stack(A, tid);
     for (unsigned g = tid; g < A.n_groups; g += kPlanThreads) {
         const Stack t = prefix_stack(A, g);
-        A.stacks[A.n_requests + g] = t;
-        work += (u64)tiles_of(A, t) * blocks_of(t);
-        pool_rows += t.rows;
+        A.stacks[g] = t;
+        work += (float)tiles_of(A, t) * (float)blocks_of(t);
+        pool_rows = add(pool_rows, t.rows);
     }
     __syncthreads();
     for (unsigned s = tid; s < A.n_requests; s += kPlanThreads) {
-        const Stack t = request_stack(A, s);
-        A.stacks[s] = t;
-        work += (u64)tiles_of(A, t) * blocks_of(t);
-        own_rows += t.rows;
+        Stack t = s < kPlanThreads ? mine : request_stack(A, s);
+        if (A.n_groups) add_prefix(A, s, t);
+        if (s < kPlanThreads) mine = t;
+        work += (float)tiles_of(A, t) * (float)blocks_of(t);
+        own_rows = add(own_rows, t.rows);
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) {
         work += __shfl_xor(work, m);
-        own_rows += __shfl_xor(own_rows, m);
-        pool_rows += __shfl_xor(pool_rows, m);
+        own_rows = add(own_rows, __shfl_xor(own_rows, m));
+        pool_rows = add(pool_rows, __shfl_xor(pool_rows, m));
     }
     if (lane == 0) {
-        s_sum[wave][0] = work;
-        s_sum[wave][1] = own_rows;
-        s_sum[wave][2] = pool_rows;
+        s_work[wave] = work;
+        s_rows[wave][0] = own_rows;
+        s_rows[wave][1] = pool_rows;
     }
-    if (tid < 3) s_base[tid] = 0;
+    if (tid < 3) S.base[tid] = 0;
     __syncthreads();
-    work = own_rows = pool_rows = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-        work += s_sum[w][0];
-        own_rows += s_sum[w][1];
-        pool_rows += s_sum[w][2];
-    }
-    // offsets that give a row to two requests: nothing is computed
-    const bool valid = own_rows <= A.n_rows && pool_rows <= A.n_rows;
-    const u64 even = (work * A.n_heads + kTarget - 1) / kTarget;
-    const unsigned chunk = (unsigned)(even > kMinBlocks ? (even < kNone ? even : kNone) : kMinBlocks);
-    for (unsigned s0 = 0; valid && s0 < n; s0 += kPlanThreads) {
-        // prefixes first: their items are the longest
-        const unsigned i = s0 + tid;
-        const unsigned s = i < A.n_groups ? A.n_requests + i : i - A.n_groups;
-        Stack t{};
-        u64 items = 0, parts = 0, joins = 0;
-        if (i < n) {
-            t = A.stacks[s];
-            const unsigned blocks = blocks_of(t);
-            t.chunk = chunk;
-            t.splits = (unsigned)(((u64)blocks + chunk - 1) / chunk);
-            const bool own = s < A.n_requests;
-            if (own && t.pool == kNone && t.splits == 0) t.splits = 1;      // writes zeros
-            if (!t.rows) t.splits = 0;
-            items = (u64)tiles_of(A, t) * t.splits;
-            const bool joined = t.splits > 1 || t.pool != kNone;
-            if (joined || !own) parts = (u64)t.rows * A.per * A.n_heads * t.splits;
-            if (joined && own) joins = t.rows;
-        }
-        // exclusive sums over the workgroup, carried from one thousand to the next
-        u64 a = items, b = parts, c = joins;
+    work = 0.f;
+    own_rows = pool_rows = 0;
 #pragma unroll
-        for (int m = 1; m < 64; m <<= 1) {
-            const u64 x = __shfl_up(a, m), y = __shfl_up(b, m), z = __shfl_up(c, m);
-            if (lane >= (unsigned)m) {
-                a += x;
-                b += y;
-                c += z;
+    for (unsigned w = 0; w < kPlanThreads / 64; ++w) {
+        work += s_work[w];
+        own_rows = add(own_rows, s_rows[w][0]);
+        pool_rows = add(pool_rows, s_rows[w][1]);
+    }
+    const float even = ceilf(work * (float)A.n_heads * (1.f / kTarget));
+    const unsigned chunk = even < (float)kMinBlocks ? kMinBlocks : even < 1e9f ? (unsigned)even : 1000000000u;
+    // offsets that give a row to two requests: nothing is computed
+    if (own_rows <= A.n_rows && pool_rows <= A.n_rows) {
+        // prefixes first: their items are the longest
+        for (unsigned g0 = 0; g0 < A.n_groups; g0 += kPlanThreads) {
+            const unsigned g = g0 + tid;
+            plan_stacks(A, g < A.n_groups ? A.stacks[g] : Stack{}, false, g < A.n_groups ? g : kNone,
+                        chunk, S);
+        }
+        for (unsigned s0 = 0; s0 < A.n_requests; s0 += kPlanThreads) {
+            const unsigned s = s0 + tid;
+            Stack t{};
+            if (s < A.n_requests) {
+                t = s0 ? request_stack(A, s) : mine;
+                if (s0 && A.n_groups) add_prefix(A, s, t);
             }
+            plan_stacks(A, t, s < A.n_requests, kNone, chunk, S);
         }
-        __syncthreads();
-        if (lane == 63) {
-            s_sum[wave][0] = a;
-            s_sum[wave][1] = b;
-            s_sum[wave][2] = c;
-        }
-        __syncthreads();
-        u64 at = s_base[0] + a - items, part = s_base[1] + b - parts, join = s_base[2] + c - joins;
-        for (unsigned w = 0; w < wave; ++w) {
-            at += s_sum[w][0];
-            part += s_sum[w][1];
-            join += s_sum[w][2];
-        }
-        if (i < n) {
-            if (parts) t.part = part;
-            A.stacks[s] = t;
-            if (s < A.n_requests) A.join0[s] = (unsigned)join;
-            const unsigned tiles = tiles_of(A, t);
-            if (at + items <= A.most_items)
-                for (unsigned j = 0; j < (unsigned)items; ++j)
-                    A.items[at + j] = uint4{s, j % tiles, j / tiles, 0};
-        }
-        __syncthreads();
-        if (tid == kPlanThreads - 1) {
-            s_base[0] = at + items;
-            s_base[1] = part + parts;
-            s_base[2] = join + joins;
-        }
-        __syncthreads();
     }
     if (tid == 0) {
         // more than the workspace holds cannot be for valid offsets
-        const bool fits = s_base[1] <= A.part_rows && s_base[0] <= A.most_items;
-        A.counts[0] = fits ? (unsigned)s_base[0] : 0;
-        A.counts[1] = fits ? (unsigned)s_base[2] : 0;
+        const bool fits = (u64)S.base[2] * A.n_heads <= A.part_rows && S.base[0] <= A.most_items &&
+            S.base[1] <= A.n_rows;
+        A.counts[0] = fits ? S.base[0] : 0;
+        A.counts[1] = fits ? S.base[1] : 0;
         A.counts[2] = 0;
     }
 }
@@ -404,7 +490,7 @@ __device__ __forceinline__ int unit_of(const AttendArgs& A, u64 first, unsigned 
 struct Range {
     unsigned nb0, most;
     u64 b0, b1;
-    __device__ Range(const AttendArgs& A, const Stack& s, unsigned last_row, unsigned split) {
+    __device__ Range(const AttendArgs& A, const Item& s, unsigned last_row, unsigned split) {
         most = (unsigned)min((long long)s.keys[1], max(0ll, (long long)s.see + last_row + 1));
         nb0 = (s.keys[0] + kBlock - 1) / kBlock;
         b0 = (u64)split * s.chunk;
@@ -415,7 +501,7 @@ struct Range {
 // Queries of one tile of 16 rows: row lane % 16, in the slots of the keys.  A scale of
 // zero or less is taken into their bits, so that scores can be compared unscaled.
 template <class T, int kDim, bool kE4m3>
-__device__ __forceinline__ void load_queries(const AttendArgs& A, const Stack& s, unsigned head,
+__device__ __forceinline__ void load_queries(const AttendArgs& A, const Item& s, unsigned head,
                                              unsigned m, unsigned quad, u32x4* q) {
     const unsigned row = m / A.per, g = m - row * A.per;
     const bool in = m < s.rows * A.per;
@@ -461,8 +547,7 @@ __device__ __forceinline__ float reference(float top, float scale) {
 // without a stop in LDS.  HBM bounds it; a wave keeps the loads of its next 16 KB in
 // flight while it computes (bf16 at dim 128: 32 keys a step).
 template <class T, int kDim, bool kE4m3, bool kWide>
-__device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, unsigned tile,
-                         unsigned split, char* lds) {
+__device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds) {
     typedef Keys<T, kDim, kE4m3> K;
     typedef typename K::P P;
     constexpr int kCols = K::kCols, kFrags = K::kFrags;
@@ -473,7 +558,7 @@ __device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, uns
     const Places<T, kDim, kE4m3> p(A);
     const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned col = p.col, quad = p.quad;
-    const unsigned total = s.rows * A.per;
+    const unsigned total = s.rows * A.per, tile = s.tile, split = s.split;
     const unsigned m = tile * 16 + col;                     // this lane's stack row
     const unsigned row = m / A.per, g = m - row * A.per;
     const unsigned last = min(total - 1, tile * 16 + 15) / A.per;
@@ -660,8 +745,7 @@ __device__ void few_rows(const AttendArgs& A, const Stack& s, unsigned head, uns
 // transposed on the way, while the products of the block before run.  From about
 // 150 rows on the products bound it, below HBM does.
 template <class T, int kDim, bool kE4m3, bool kWide, int kQ>
-__device__ void many_rows(const AttendArgs& A, const Stack& s, unsigned head, unsigned tile,
-                          unsigned split, char* lds) {
+__device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds) {
     typedef Keys<T, kDim, kE4m3> K;
     typedef typename K::P P;
     constexpr int kCols = K::kCols, kFrags = K::kFrags;
@@ -670,7 +754,7 @@ __device__ void many_rows(const AttendArgs& A, const Stack& s, unsigned head, un
     const Places<T, kDim, kE4m3> p(A);
     const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned col = p.col, quad = p.quad;
-    const unsigned total = s.rows * A.per;
+    const unsigned total = s.rows * A.per, tile = s.tile, split = s.split;
     const unsigned m0 = tile * 64 * kQ, mw = m0 + wave * 16 * kQ;   // the tile's, the wave's first row
     const unsigned last = min(total - 1, m0 + 64 * kQ - 1) / A.per;
     const Range range(A, s, last, split);
@@ -863,99 +947,112 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
     for (unsigned turn = 0; it < n; turn ^= 1) {
         if (threadIdx.x == 0) s_ticket[turn] = gridDim.x + atomicAdd(&A.counts[2], 1u);
         const unsigned head = (unsigned)(it % A.n_heads);
-        const uint4 item = A.items[it / A.n_heads];
-        const Stack s = A.stacks[item.x];
-        const unsigned rows = tile_rows(A, s);
-        if (rows == 16) few_rows<T, kDim, kE4m3, kWide>(A, s, head, item.y, item.z, lds);
-        else if (rows == 64) many_rows<T, kDim, kE4m3, kWide, 1>(A, s, head, item.y, item.z, lds);
-        else many_rows<T, kDim, kE4m3, kWide, 2>(A, s, head, item.y, item.z, lds);
+        const Item s = A.items[it / A.n_heads];
+        if (s.tile_rows == 16) few_rows<T, kDim, kE4m3, kWide>(A, s, head, lds);
+        else if (s.tile_rows == 64) many_rows<T, kDim, kE4m3, kWide, 1>(A, s, head, lds);
+        else many_rows<T, kDim, kE4m3, kWide, 2>(A, s, head, lds);
         it = s_ticket[turn];
     }
 }
 
-// Joins the parts of rows that several items share.  A workgroup takes a row and query
-// head at a time: all lanes read the parts' references and sums, then each wave adds up
-// every fourth part, kDim / 64 columns a lane, and the four meet in LDS.  With the parts
-// one after the other in one wave, 128 parts of a long row took 81 us.
+// Joins the parts of rows that several items share: kTeam waves take a row and query
+// head, wave w every kTeam-th part from w on, kDim / 64 columns a lane; a team's waves
+// meet in LDS.  Reads that wait for each other bound it (parts come from other XCDs'
+// caches), so the parts are read along with their references, eight at a time, and
+// small batches get a workgroup a row (one wave took 81 us for 128 parts of 32 rows).
+template <class T, int kDim, int kTeam>
+__device__ __forceinline__ void join_row(const AttendArgs& A, u64 w, float (*s_x)[kDim], float2* s_ml) {
+    constexpr int kCols = kDim / 64;
+    const unsigned lane = threadIdx.x % 64, member = kTeam == 1 ? 0 : threadIdx.x / 64;
+    const unsigned heads = A.n_heads * A.per;
+    const JoinRow r = A.joins[w / heads];
+    const unsigned qh = (unsigned)(w % heads), head = qh / A.per, g = qh - head * A.per;
+    const u64 first0 = r.first[0] + (u64)head * r.splits[0] * r.total[0] + g;
+    const u64 first1 = r.first[1] + (u64)head * r.splits[1] * r.total[1] + g;
+    const unsigned parts = r.splits[0] + r.splits[1];
+    float top = -INFINITY, sum = 0.f, x[kCols];
+#pragma unroll
+    for (int c = 0; c < kCols; ++c) x[c] = 0.f;
+    constexpr int kAtOnce = kDim > 128 ? 4 : 8;
+    for (unsigned i0 = member; i0 < parts; i0 += kTeam * kAtOnce) {
+        float2 ml[kAtOnce];
+        float y[kAtOnce][kCols];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const unsigned i = min(i0 + k * kTeam, parts - 1);
+            const u64 at = i < r.splits[0] ? first0 + (u64)i * r.total[0]
+                                           : first1 + (u64)(i - r.splits[0]) * r.total[1];
+            ml[k] = A.part_ml[at];
+            const float* from = &A.part_o[at * kDim + lane * kCols];
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) y[k][c] = from[c];
+        }
+        float best = top;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            if (i0 + k * kTeam >= parts) ml[k] = float2{-INFINITY, 0.f};
+            best = fmaxf(best, ml[k].x);
+        }
+        const float ref = best == -INFINITY ? 0.f : best, shrink = exp2f(top - ref);
+        top = best;
+        sum *= shrink;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) x[c] *= shrink;
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const float f = exp2f(ml[k].x - ref);
+            sum += ml[k].y * f;
+            // columns behind dim, and of a part that is not there, may hold anything
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) x[c] += i0 + k * kTeam < parts ? y[k][c] * f : 0.f;
+        }
+    }
+    if constexpr (kTeam > 1) {
+        if (lane == 0) s_ml[member] = float2{top, sum};
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) s_x[member][lane * kCols + c] = x[c];
+        __syncthreads();
+        if (member == 0) {
+#pragma unroll
+            for (int k = 1; k < kTeam; ++k) {
+                const float2 ml = s_ml[k];
+                const float best = fmaxf(top, ml.x), ref = best == -INFINITY ? 0.f : best;
+                const float a = exp2f(top - ref), b = exp2f(ml.x - ref);
+                top = best;
+                sum = sum * a + ml.y * b;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) x[c] = x[c] * a + s_x[k][lane * kCols + c] * b;
+            }
+        }
+    }
+    if (member == 0) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        unsigned short* to = reinterpret_cast<unsigned short*>(A.out + (u64)r.row * A.out_row +
+                                                               (u64)qh * A.out_head) + lane * kCols;
+        if (lane * kCols < A.dim) {
+            if constexpr (kCols == 1) {
+                *to = (unsigned short)T::pack(x[0] * inv, 0.f);
+            } else {
+#pragma unroll
+                for (int c = 0; c < kCols; c += 2)
+                    reinterpret_cast<unsigned*>(to)[c / 2] = T::pack(x[c] * inv, x[c + 1] * inv);
+            }
+        }
+        if (A.lse && lane == 0) A.lse[(u64)r.row * heads + qh] = (top + log2f(sum)) * 0.6931471805599453f;
+    }
+    if constexpr (kTeam > 1) __syncthreads();
+}
+
 template <class T, int kDim>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
-    constexpr int kCols = kDim / 64;
-    __shared__ float s_w[256], s_top[4], s_sum[4], s_x[3][kDim];
-    const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const unsigned heads = A.n_heads * A.per;
-    const u64 n = (u64)A.counts[1] * heads;
-    for (u64 w = blockIdx.x; w < n; w += gridDim.x) {
-        const unsigned j = (unsigned)(w / heads), qh = (unsigned)(w % heads);
-        const unsigned r = wave_search(A.n_requests, j, [&](unsigned i) { return A.join0[i]; });
-        const Stack own = A.stacks[r];
-        const unsigned t = own.row0 + (j - A.join0[r]);
-        const unsigned head = qh / A.per, g = qh - head * A.per;
-        const Stack pool = A.stacks[own.pool == kNone ? r : own.pool];
-        const u64 own_total = (u64)own.rows * A.per, pool_total = (u64)pool.rows * A.per;
-        const u64 own_first = own.part + (u64)head * own.splits * own_total + (u64)(t - own.row0) * A.per + g;
-        const u64 pool_first = pool.part + (u64)head * pool.splits * pool_total + (u64)(t - pool.row0) * A.per + g;
-        // offsets that break the rules can put a request outside its group's rows
-        const bool in_pool = own.pool != kNone && t >= pool.row0 && t - pool.row0 < pool.rows;
-        const unsigned parts = own.splits + (in_pool ? pool.splits : 0);
-        auto part = [&](unsigned i) {
-            return i < own.splits ? own_first + i * own_total : pool_first + (i - own.splits) * pool_total;
-        };
-        float top = -INFINITY, sum = 0.f, x[kCols];
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) x[c] = 0.f;
-        for (unsigned i0 = 0; i0 < parts; i0 += 256) {
-            const unsigned i = i0 + threadIdx.x;
-            const float2 ml = i < parts ? A.part_ml[part(i)] : float2{-INFINITY, 0.f};
-            float best = ml.x;
-#pragma unroll
-            for (int m = 32; m; m >>= 1) best = fmaxf(best, __shfl_xor(best, m));
-            if (lane == 0) s_top[wave] = best;
-            __syncthreads();
-            best = fmaxf(fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3])), top);
-            const float ref = best == -INFINITY ? 0.f : best, shrink = exp2f(top - ref);
-            const float weight = exp2f(ml.x - ref);
-            s_w[threadIdx.x] = weight;
-            float part_sum = ml.y * weight;
-#pragma unroll
-            for (int m = 32; m; m >>= 1) part_sum += __shfl_xor(part_sum, m);
-            if (lane == 0) s_sum[wave] = part_sum;
-            __syncthreads();
-            sum = sum * shrink + ((s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]));
-            top = best;
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) x[c] *= shrink;
-            const unsigned k = min(256u, parts - i0);
-#pragma unroll 8
-            for (unsigned i = wave; i < k; i += 4) {
-                const float* from = &A.part_o[part(i0 + i) * kDim + lane * kCols];
-                const float f = s_w[i];
-#pragma unroll
-                for (int c = 0; c < kCols; ++c) x[c] += lane * kCols < A.dim ? from[c] * f : 0.f;
-            }
-            __syncthreads();
-        }
-        if (wave) {
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) s_x[wave - 1][lane * kCols + c] = x[c];
-        }
-        __syncthreads();
-        if (wave == 0) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-            for (int c = 0; c < kCols; ++c)
-                x[c] = (((x[c] + s_x[0][lane * kCols + c]) + s_x[1][lane * kCols + c]) + s_x[2][lane * kCols + c]) * inv;
-            unsigned short* to = reinterpret_cast<unsigned short*>(A.out + (u64)t * A.out_row + (u64)qh * A.out_head) + lane * kCols;
-            if (lane * kCols < A.dim) {
-                if constexpr (kCols == 1) {
-                    *to = (unsigned short)T::pack(x[0], 0.f);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < kCols; c += 2) reinterpret_cast<unsigned*>(to)[c / 2] = T::pack(x[c], x[c + 1]);
-                }
-            }
-            if (A.lse && lane == 0) A.lse[(u64)t * heads + qh] = (top + log2f(sum)) * 0.6931471805599453f;
-        }
-        __syncthreads();
+    __shared__ float s_x[4][kDim];
+    __shared__ float2 s_ml[4];
+    const u64 n = (u64)A.counts[1] * (A.n_heads * A.per);
+    if (n <= gridDim.x) {
+        if (blockIdx.x < n) join_row<T, kDim, 4>(A, blockIdx.x, s_x, s_ml);
+    } else {
+        for (u64 w = blockIdx.x * 4 + threadIdx.x / 64; w < n; w += gridDim.x * 4)
+            join_row<T, kDim, 1>(A, w, s_x, s_ml);
     }
 }
 
@@ -964,25 +1061,25 @@ u64 up(u64 x) { return (x + 255) & ~255ull; }
 
 // Partial rows at most: every row once for its own tokens and once for a shared
 // prefix, and a tile for each split beyond a stack's first; there are at most
-// kTarget of those, as every one but a stack's last has its share of the work.
-u64 part_rows(u64 n_rows, u64 n_q_heads) {
-    return 2 * n_rows * n_q_heads + (u64)kTarget * kMostRows;
-}
+// kTarget of those (and a few for the work's rounding), as every one but a stack's
+// last has its share of the work.
+constexpr u64 kMoreItems = kTarget + 16;
+u64 part_rows(u64 n_rows, u64 n_q_heads) { return 2 * n_rows * n_q_heads + kMoreItems * kMostRows; }
 
 // Items per head at most: a tile of every 16 rows and every stack's last one, once for
 // own tokens and once for prefixes, and the splits.
-u64 most_items(u64 n_rows, u64 n_stacks, u64 per) { return 2 * (n_rows * per / 16) + n_stacks + kTarget; }
+u64 most_items(u64 n_rows, u64 n_stacks, u64 per) { return 2 * (n_rows * per / 16) + n_stacks + kMoreItems; }
 
 struct Layout {
-    u64 items, join0, stacks, ml, o, bytes;
+    u64 items, joins, stacks, ml, o, bytes;
 };
 Layout layout_of(u64 n_rows, u64 n_requests, u64 n_groups, u64 n_heads, u64 per, unsigned dim) {
     Layout l;
     const u64 n = n_requests + n_groups, rows = part_rows(n_rows, n_heads * per);
     l.items = 256;
-    l.join0 = up(l.items + sizeof(uint4) * most_items(n_rows, n, per));
-    l.stacks = up(l.join0 + 4 * n_requests);
-    l.ml = up(l.stacks + sizeof(Stack) * n);
+    l.joins = up(l.items + sizeof(Item) * most_items(n_rows, n, per));
+    l.stacks = up(l.joins + sizeof(JoinRow) * n_rows);
+    l.ml = up(l.stacks + sizeof(Stack) * n_groups);
     l.o = up(l.ml + 8 * rows);
     l.bytes = l.o + 4 * rows * padded(dim);
     return l;
@@ -1014,8 +1111,8 @@ ss_status attend_args(const ss_kv_cache* c, const ss_batch* b, uint32_t type, ui
     if (s != SS_OK) return s;
     if (n_q_heads < 1 || n_q_heads > 65536 || n_q_heads % c->n_heads)
         return set_err(SS_ERR_ARG, "n_q_heads must be a multiple of the cache's n_heads, at most 65536");
-    if ((u64)b->n_rows * n_q_heads >= (1ull << 31))
-        return set_err(SS_ERR_ARG, "n_rows * n_q_heads must be below 2^31");
+    if ((u64)b->n_rows * n_q_heads >= (1ull << 30))
+        return set_err(SS_ERR_ARG, "n_rows * n_q_heads must be below 2^30");
     return SS_OK;
 }
 
@@ -1108,8 +1205,8 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     A.q_flip = scale < 0.f ? 0x80008000u : 0u;
     char* ws = static_cast<char*>(workspace);
     A.counts = reinterpret_cast<unsigned*>(ws);
-    A.items = reinterpret_cast<uint4*>(ws + l.items);
-    A.join0 = reinterpret_cast<unsigned*>(ws + l.join0);
+    A.items = reinterpret_cast<Item*>(ws + l.items);
+    A.joins = reinterpret_cast<JoinRow*>(ws + l.joins);
     A.most_items = most_items(rows, batch->n_requests + batch->n_groups, n_q_heads / cache->n_heads);
     A.stacks = reinterpret_cast<Stack*>(ws + l.stacks);
     A.part_ml = reinterpret_cast<float2*>(ws + l.ml);

@@ -133,7 +133,7 @@ def test_attention(change, msg):
 
 
 def test_attention_of_too_many_rows():
-    refused("2\\^31", attend, None, batch(n_rows=1 << 30))
+    refused("2\\^30", attend, None, batch(n_rows=1 << 28))
 
 
 @pytest.mark.parametrize("change,msg", [
@@ -141,7 +141,8 @@ def test_attention_of_too_many_rows():
     (dict(b=P + 4), "aligned"), (dict(rank=0), "rank"), (dict(rank=12), "rank"), (dict(rank=136), "rank"),
     (dict(n_in=0), "n_in"), (dict(n_in=60), "n_in"), (dict(n_out=1 << 24), "n_out"),
     (dict(type=B.SS_E4M3), "SS_BF16 or SS_F16"), (dict(a_unit_bytes=4104), "multiples of 16"),
-    (dict(b_unit_bytes=1 << 31), "below 2"), (dict(a_unit_bytes=1024), "does not fit")])
+    (dict(b_unit_bytes=1 << 31), "below 2"),
+    (dict(rank=128, n_out=(1 << 24) - 8, capacity_units=1), "too large"), (dict(a_unit_bytes=1024), "does not fit")])
 def test_adapters(change, msg):
     refused(msg, add, adapters(**change))
     assert B.adapter_add_workspace(adapters(**change), 4, 2) == 0
