@@ -88,20 +88,29 @@ __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0, 0, 0, 0};
     const u32x4 zero = {0, 0, 0, 0};
-    for (unsigned k = k0 + wave * 32; k < k1; k += 128) {
-        const unsigned at = k + quad * 8;
-        const bool in = at < k1;
-        const u64 off = (u64)(in ? at : k0) * 2;
-        u32x4 xf = *reinterpret_cast<const u32x4*>(xr + off);
-        if (!in || col >= rows) xf = zero;
-        u32x4 af[kTiles];
+    // steps of 32 elements, as many reads in flight as registers hold
+    constexpr int kSteps = kTiles == 1 ? 8 : kTiles == 2 ? 4 : 2;
+#pragma unroll 1
+    for (unsigned k = k0 + wave * 32; k < k1; k += 128 * kSteps) {
+        u32x4 xf[kSteps], af[kSteps][kTiles];
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-            af[t] = *reinterpret_cast<const u32x4*>(ar[t] + off);
-            if (!in || t * 16 + col >= A.rank) af[t] = zero;
+        for (int u = 0; u < kSteps; ++u) {
+            const unsigned at = k + 128 * u + quad * 8;
+            const u64 off = (u64)(at < k1 ? at : k0) * 2;
+            xf[u] = *reinterpret_cast<const u32x4*>(xr + off);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) af[u][t] = *reinterpret_cast<const u32x4*>(ar[t] + off);
         }
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) acc[t] = T::mma(af[t], xf, acc[t]);
+        for (int u = 0; u < kSteps; ++u) {
+            const bool in = k + 128 * u + quad * 8 < k1;
+            if (!in || col >= rows) xf[u] = zero;
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                if (!in || t * 16 + col >= A.rank) af[u][t] = zero;
+                acc[t] = T::mma(af[u][t], xf[u], acc[t]);
+            }
+        }
     }
     if (wave) {
 #pragma unroll
@@ -272,13 +281,123 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
     }
 }
 
+// Decoding: a workgroup per tile of up to four rows and A.cols columns.  With so few rows
+// B's bytes bound it, so they are read as they lie, 16 bytes a lane, and multiplied in
+// 32 bits: a column's ranks are in kSplit = rank / 8 lanes next to each other, each of
+// which takes eight columns in a row, so that the sums need log2(kSplit) exchanges and
+// leave in 16 bytes.  8 KB are in flight per wave while the 8 KB before are used
+// (as matrix products with two thirds of the lanes' reads doubled: 256 adapters of rank
+// 16 by 14,336 columns in 50 us).
+constexpr unsigned kFewRows = 4;
+template <class T, int kSplit>
+__global__ __launch_bounds__(kThreads, 3) void k_adapter_out_few(AdapterArgs A) {
+    constexpr unsigned kCols = 512 / kSplit;            // columns of a wave's round
+    unsigned r, row0;
+    const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
+    const unsigned rows = tile_of<kFewRows>(A, blockIdx.x / parts, &r, &row0);
+    if (!rows) return;
+    const int unit = adapter_of(A, r);
+    if (unit < 0 && A.base == A.out) return;
+    const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned c = lane % kSplit, col = lane / kSplit * 8;          // ranks 8 c .., columns col ..
+    const unsigned n0 = blockIdx.x % parts * A.cols + wave * kCols;
+    const unsigned n1 = min(A.n_out, blockIdx.x % parts * A.cols + A.cols);
+    if (unit < 0) {
+        for (unsigned n = n0 + lane * 8; n < n1; n += 4 * kCols)
+            if (lane * 8 < kCols)
+                for (unsigned t = 0; t < rows; ++t)
+                    *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + t) * A.out_row + (u64)n * 2) =
+                        *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + (u64)n * 2);
+        return;
+    }
+    const char* const bm = A.b + (u64)unit * A.b_unit;
+    auto load = [&](unsigned nw, u32x4* b) {
+        const unsigned at = nw + col < n1 ? ((nw + col) * kSplit + c) * 16 : c * 16;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) b[j] = *reinterpret_cast<const u32x4*>(bm + (at + j * kSplit * 16));
+    };
+    u32x4 b[2][8];
+    if (n0 < n1) load(n0, b[0]);
+    const float scale = A.scales ? A.scales[r] : 1.f;
+    float h[kFewRows][8];
+#pragma unroll
+    for (unsigned t = 0; t < kFewRows; ++t) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[t][j] = 0.f;
+        if (t < rows)
+            for (unsigned p = 0; p < A.pieces; ++p) {
+                const float* from = A.low + ((u64)p * A.n_rows + row0 + t) * A.rank + 8 * c;
+                const f32x4 u = *reinterpret_cast<const f32x4*>(from);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(from + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    h[t][j] += u[j];
+                    h[t][4 + j] += v[j];
+                }
+            }
+    }
+    auto use = [&](unsigned nw, const u32x4* b) {
+        const unsigned n = nw + col;
+#pragma unroll
+        for (unsigned t = 0; t < kFewRows; ++t) {
+            if (t >= rows) break;
+            u32x4 base = {0, 0, 0, 0};
+            if (c == 0 && n < n1)
+                base = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + (u64)n * 2);
+            float y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                y[j] = 0.f;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    y[j] = fmaf(T::lo(b[j][k]), h[t][2 * k], y[j]);
+                    y[j] = fmaf(T::hi(b[j][k]), h[t][2 * k + 1], y[j]);
+                }
+            }
+#pragma unroll
+            for (int m = kSplit / 2; m; m >>= 1)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[j] += __shfl_xor(y[j], m);
+            if (c == 0 && n < n1) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    base[j] = T::pack(T::lo(base[j]) + scale * y[2 * j], T::hi(base[j]) + scale * y[2 * j + 1]);
+                *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + t) * A.out_row + (u64)n * 2) = base;
+            }
+        }
+    };
+#pragma unroll 1
+    for (unsigned nw = n0; nw < n1; nw += 8 * kCols) {
+        if (nw + 4 * kCols < n1) load(nw + 4 * kCols, b[1]);
+        use(nw, b[0]);
+        if (nw + 4 * kCols >= n1) break;
+        if (nw + 8 * kCols < n1) load(nw + 8 * kCols, b[0]);
+        use(nw + 4 * kCols, b[1]);
+    }
+}
+
+template <class T, int kSplit>
+void out_few_launch(const AdapterArgs& A, hipStream_t st) {
+    // two rounds a wave: a workgroup reads its way to the adapter before it streams, and
+    // more rounds leave too few workgroups
+    AdapterArgs B = A;
+    B.cols = 2 * 4 * 512 / kSplit;
+    const unsigned tiles = A.n_rows / kFewRows + A.n_requests;
+    hipLaunchKernelGGL((k_adapter_out_few<T, kSplit>), dim3((A.n_out + B.cols - 1) / B.cols * tiles),
+                       dim3(kThreads), 0, st, B);
+}
+
 template <class T, int kSub>
 void out_launch(const AdapterArgs& A, hipStream_t st) {
     const unsigned tiles = A.n_rows / (16 * kSub) + A.n_requests;
     // a workgroup reads its way to the adapter before it streams, so it takes several
-    // 512 columns once there are 1,024 workgroups
+    // 512 columns where there are more workgroups than run at a time
     const unsigned pieces = (A.n_out + kOutCols - 1) / kOutCols;
-    const unsigned each = std::max(1u, std::min<unsigned>(pieces, (unsigned)((u64)pieces * tiles / 1024)));
+    // (all at once: two or three a compute unit), of about the same length each
+    const unsigned most = kSub == 1 ? 768 : 512;
+    const unsigned rounds = (unsigned)(((u64)pieces * tiles + 4 * most - 1) / (4 * most));
+    const unsigned want = std::max(1u, (unsigned)((u64)most * rounds / tiles));      // pieces' groups
+    const unsigned each = std::max(1u, (pieces + want - 1) / want);
     AdapterArgs B = A;
     B.cols = kOutCols * each;
     const dim3 grid((pieces + each - 1) / each * tiles), block(kThreads);
@@ -296,6 +415,16 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
         case 3:
         case 4: hipLaunchKernelGGL((k_adapter_in<T, 4>), in, block, 0, st, A); break;
         default: hipLaunchKernelGGL((k_adapter_in<T, 8>), in, block, 0, st, A); break;
+    }
+    // up to two rows a request as a rule: no product of 16 rows is worth its reads
+    if (A.n_rows <= 2ull * A.n_requests) {
+        switch (A.rank) {
+            case 8: return out_few_launch<T, 1>(A, st);
+            case 16: return out_few_launch<T, 2>(A, st);
+            case 32: return out_few_launch<T, 4>(A, st);
+            case 64: return out_few_launch<T, 8>(A, st);
+            case 128: return out_few_launch<T, 16>(A, st);
+        }
     }
     // tiles of 32 rows where requests fill them: B is read half as often
     if (A.n_rows >= 24ull * A.n_requests) out_launch<T, 2>(A, st);
@@ -367,7 +496,8 @@ ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, con
         (s = rows_args("base", base, rows, 1, n_out, base_stride, n_out, false)) != SS_OK ||
         (s = rows_args("out", out, rows, 1, n_out, out_stride, n_out, true)) != SS_OK)
         return s;
-    if ((rows / kTile + batch->n_requests) * ((n_out + kOutCols - 1) / kOutCols) >= (1ull << 31))
+    // workgroups of the kernel that has most
+    if ((rows / kFewRows + batch->n_requests) * ((n_out + 255) / 256) >= (1ull << 31))
         return set_err(SS_ERR_ARG, "n_rows * n_out is too large");
     const u64 x_bytes = rows_bytes(rows, 1, n_in, x_stride, 0);
     const u64 base_bytes = rows_bytes(rows, 1, n_out, base_stride, 0);

@@ -22,8 +22,6 @@ struct Bf16 {
     }
     static __device__ float lo(unsigned w) { return __uint_as_float(w << 16); }
     static __device__ float hi(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
-    // of a value in the upper half of a word
-    static __device__ bool is_infinite(unsigned bits) { return (bits & 0x7fffffffu) == 0x7f800000u; }
     // two e4m3 codes (the word's lower or upper half), exactly
     template <bool kHigh>
     static __device__ unsigned from_e4m3(unsigned codes) {
@@ -42,7 +40,6 @@ struct F16 {
     }
     static __device__ float lo(unsigned w) { return (float)__builtin_bit_cast(f16x2, w)[0]; }
     static __device__ float hi(unsigned w) { return (float)__builtin_bit_cast(f16x2, w)[1]; }
-    static __device__ bool is_infinite(unsigned bits) { return (bits & 0x7fffffffu) == 0x7c000000u; }
     template <bool kHigh>
     static __device__ unsigned from_e4m3(unsigned codes) {
         return __builtin_bit_cast(unsigned,
