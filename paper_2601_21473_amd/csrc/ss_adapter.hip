@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
                     for (int j = 0; j < 4; ++j)
                         w[j] = T::pack(T::lo(w[j]) + f * acc[s][2 * j][i], T::hi(w[j]) + f * acc[s][2 * j + 1][i]);
                 }
-                *reinterpret_cast<u32x4*>(A.out + (u64)(row0 + t) * A.out_row + (u64)n * 2) = w;
+                store_past(w, A.out + (u64)(row0 + t) * A.out_row + (u64)n * 2);
             }
         load_base(n + kOutCols, base);
     }

@@ -23,6 +23,7 @@ constexpr unsigned kNone = 0xffffffffu;
 constexpr unsigned kBlock = 64;             // keys of one step of an item
 constexpr unsigned kTarget = 1024;          // items that a call is split into at least, if it can
 constexpr unsigned kMinBlocks = 4;          // and key blocks that an item has at least
+constexpr unsigned kXcds = 8;               // of the card, each with its own L2
 constexpr unsigned kMostRows = 128;         // rows of the largest tile
 
 struct Stack {
@@ -79,7 +80,8 @@ struct AttendArgs {
     float scale;                                // |scale| log2(e), 1 for a scale of 0
     unsigned q_keep, q_flip;                    // queries' bits that count, and that turn
     // workspace
-    unsigned* counts;                           // items per head, rows to join, items taken
+    unsigned* counts;                           // items per head, rows to join
+    unsigned* taken;                            // [kXcds] items taken behind the first
     Item* items;                                // [most_items]
     JoinRow* joins;                             // [n_rows]
     Stack* stacks;                              // [n_groups] of the prefixes
@@ -339,8 +341,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
             S.base[1] <= A.n_rows;
         A.counts[0] = fits ? S.base[0] : 0;
         A.counts[1] = fits ? S.base[1] : 0;
-        A.counts[2] = 0;
     }
+    if (tid < kXcds) A.taken[tid] = 0;
 }
 
 constexpr int kWaves = 4;
@@ -348,6 +350,15 @@ constexpr int kWaves = 4;
 // the reference then stays for most blocks, and a block's maximum need not be known
 // to all lanes of a row.  2^8 is exact in every type and far from their ranges.
 constexpr float kSlack = 8.f;
+
+// The lane, of which the compiler knows nothing: what follows from it is worked out for
+// each item anew and not kept in registers beside the other tile sizes' values (they
+// spilled up to 60 registers).
+__device__ __forceinline__ unsigned own_lane() {
+    unsigned lane = threadIdx.x % 64;
+    asm volatile("" : "+v"(lane));
+    return lane;
+}
 
 // A lane's share of 16 keys and values as they come from memory, and where it lies.
 // Products want S^T = K Q^T and O^T = V^T P^T with 16 x 16 x 32 products:
@@ -398,8 +409,7 @@ struct Places {
     typedef Keys<T, kDim, kE4m3> K;
     unsigned col, quad;
     unsigned kd[K::kLoads], vd;     // byte offsets inside a row, 0 behind dim
-    __device__ Places(const AttendArgs& A) {
-        const unsigned lane = threadIdx.x % 64;
+    __device__ Places(const AttendArgs& A, unsigned lane) {
         col = lane % 16;
         quad = lane / 16;
 #pragma unroll
@@ -555,8 +565,8 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
     constexpr unsigned kSteps = 4 / kSub;               // steps of a block
     float* lds_o = reinterpret_cast<float*>(lds);
     float2* lds_ml = reinterpret_cast<float2*>(lds + kWaves * 16 * (kDim + 4) * 4);
-    const Places<T, kDim, kE4m3> p(A);
-    const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const Places<T, kDim, kE4m3> p(A, lane);
     const unsigned col = p.col, quad = p.quad;
     const unsigned total = s.rows * A.per, tile = s.tile, split = s.split;
     const unsigned m = tile * 16 + col;                     // this lane's stack row
@@ -735,25 +745,163 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
             A.part_ml[part0 + m] = float2{best, l};
         }
     }
-    __syncthreads();            // the next item's LDS
 }
 
-// 64 kQ rows and a range of keys: each wave has 16 kQ rows and all keys.  A block of
-// 64 keys and values goes through LDS once for the four waves, in the layout of the
-// products' operands (a fragment is 64 lanes x 16 bytes, so neither side has bank
-// conflicts); wave w brings the block's keys 16 w .. 16 w + 15, converted and
-// transposed on the way, while the products of the block before run.  From about
-// 150 rows on the products bound it, below HBM does.
-template <class T, int kDim, bool kE4m3, bool kWide, int kQ>
-__device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds) {
+// A block of 64 keys and values in LDS, in the layout of the products' operands, and
+// how it gets there.  A fragment of keys is 64 lanes x 16 bytes, read without bank
+// conflicts.  Wave w brings the block's keys 16 w .. 16 w + 15 while the products of the
+// block before run.
+// Through registers (e4m3, which is converted on the way, and dims that are filled
+// up): values are transposed by byte permutes, so their fragments are like the keys'.
+template <class T, int kDim, bool kE4m3, bool kWide>
+struct ThroughRegisters {
     typedef Keys<T, kDim, kE4m3> K;
-    typedef typename K::P P;
-    constexpr int kCols = K::kCols, kFrags = K::kFrags;
-    constexpr unsigned kKeyBytes = 4 * kFrags * 1024, kValueBytes = 2 * kCols * 1024;
-    constexpr unsigned kBuffer = kKeyBytes + kValueBytes + 512;
-    const Places<T, kDim, kE4m3> p(A);
-    const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const unsigned col = p.col, quad = p.quad;
+    static constexpr int kCols = K::kCols, kFrags = K::kFrags;
+    static constexpr unsigned kKeyBytes = 4 * kFrags * 1024, kValueBytes = 2 * kCols * 1024;
+    static constexpr unsigned kBuffer = kKeyBytes + kValueBytes + 512;
+    Places<T, kDim, kE4m3> p;
+    K x;
+    unsigned lane, wave;
+    __device__ ThroughRegisters(const AttendArgs& A, unsigned l, unsigned w) : p(A, l), lane(l), wave(w) {}
+    // Asks for the wave's keys of the block at key0 into buffer `to`.
+    __device__ void ask(const AttendArgs& A, unsigned head, int unit, unsigned key0, char*) {
+        load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * wave, key0 + 16 * wave, x);
+    }
+    // Has them in the buffer, for all waves; `there`: the block's keys that are tokens.
+    __device__ void arrive(const AttendArgs& A, u64 there, char* to) {
+        char* const lv = to + kKeyBytes;
+        float* const ls = reinterpret_cast<float*>(lv + kValueBytes);
+        if (there != ~0ull) {
+            const unsigned bits = (unsigned)(there >> (16 * wave + 4 * p.quad)) & 15u;
+            clear_values(x, bits);
+            if constexpr (kE4m3) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (!(bits >> c & 1)) x.ks[c] = x.vs[c] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+            u32x4 kf = x.key(f);
+            if (A.dim != kDim && K::slot_dim(f, p.quad) >= A.dim) kf = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<u32x4*>(to + ((wave * kFrags + f) * 64 + lane) * 16) = kf;
+        }
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            const unsigned sel = c % 2 ? 0x07060302u : 0x05040100u;
+            const u32x2 vf = {__builtin_amdgcn_perm(x.value(1, c / 2), x.value(0, c / 2), sel),
+                              __builtin_amdgcn_perm(x.value(3, c / 2), x.value(2, c / 2), sel)};
+            *reinterpret_cast<u32x2*>(lv + (((wave / 2) * kCols + c) * 64 + lane) * 16 + (wave % 2) * 8) = vf;
+        }
+        if constexpr (kE4m3) {
+            if (p.col == 0) {
+                *reinterpret_cast<f32x4*>(ls + 16 * wave + 4 * p.quad) = x.ks;
+                *reinterpret_cast<f32x4*>(ls + 64 + 16 * wave + 4 * p.quad) = x.vs;
+            }
+        }
+        __syncthreads();
+    }
+    // Fragment c of the values of keys 32 h ..; row r of a lane's product is the column:
+    __device__ u32x4 value(const char* from, int h, int c) const {
+        return *reinterpret_cast<const u32x4*>(from + kKeyBytes + ((h * kCols + c) * 64 + lane) * 16);
+    }
+    static constexpr __host__ __device__ unsigned column(unsigned quad, int r, int c) { return (4 * quad + r) * kCols + c; }
+    __device__ f32x4 scales(const char* from, unsigned what, unsigned key) const {
+        return *reinterpret_cast<const f32x4*>(from + kKeyBytes + kValueBytes + 4 * (64 * what + key));
+    }
+};
+
+// Straight from memory into LDS, without registers (16-bit caches of the full dim): a
+// wave's read puts lane l's 16 bytes at l * 16, so the layout lies in which bytes
+// each lane asks for.  Values keep their rows, 16-byte pieces c of key k at c ^ 2 (k % 8)
+// (16 rows' 32 bytes would else share their banks), and are transposed when read:
+// of four rows that 16 lanes point at, each lane gets one column.
+template <class T, int kDim, bool kWide>
+struct Straight {
+    static constexpr int kCols = kDim / 16, kFrags = kDim / 32, kPieces = kDim / 8;
+    static constexpr unsigned kKeyBytes = 64 * kDim * 2;
+    static constexpr unsigned kBuffer = 2 * kKeyBytes;
+    static constexpr unsigned kTurn = kPieces < 16 ? 3 : 7;       // pieces are turned in pairs
+    unsigned lane, wave, col, quad;
+    __device__ Straight(const AttendArgs&, unsigned l, unsigned w) : lane(l), wave(w), col(l % 16), quad(l / 16) {}
+    static __device__ void bring(const char* from, char* to) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                         (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    }
+    static __device__ unsigned turn(unsigned key) { return 2 * (key & kTurn); }
+    __device__ void ask(const AttendArgs& A, unsigned head, int unit, unsigned key0, char* to) {
+        const unsigned mask = (1u << A.shift) - 1u;
+        const u64 head_off = (u64)head * A.head_bytes;
+        const unsigned first = key0 + 16 * wave;
+        // the wave's keys: fragments, then rows of values (kPieces lanes a row)
+        char* const lk = to + wave * kFrags * 1024;
+        char* const lv = to + kKeyBytes + wave * (16 * kDim * 2);
+        constexpr unsigned kRowsAtOnce = 64 / kPieces;
+        if constexpr (kWide) {
+            const int u0 = __builtin_amdgcn_readlane(unit, 16 * wave);
+            const u64 u = u0 < 0 ? 0 : u0;
+            const unsigned tb = (unsigned)A.token_bytes;
+            const u64 slot = (u64)(first & mask) * A.token_bytes + head_off;
+            const char* const kb = A.k + u * A.k_unit + slot;
+            const char* const vb = A.v + u * A.v_unit + slot;
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) bring(kb + (col * tb + 64 * f + 16 * quad), lk + f * 1024);
+#pragma unroll
+            for (unsigned n = 0; n < 16 / kRowsAtOnce; ++n) {
+                const unsigned key = n * kRowsAtOnce + lane / kPieces;
+                bring(vb + (key * tb + 16 * (lane % kPieces ^ turn(key))), lv + n * 1024);
+            }
+        } else {
+            const int safe = unit < 0 ? 0 : unit;
+            const u64 ku = (u64)__shfl(safe, 16 * wave + col);
+            const char* const kb = A.k + ku * A.k_unit + (u64)((first + col) & mask) * A.token_bytes + head_off;
+#pragma unroll
+            for (int f = 0; f < kFrags; ++f) bring(kb + (64 * f + 16 * quad), lk + f * 1024);
+#pragma unroll
+            for (unsigned n = 0; n < 16 / kRowsAtOnce; ++n) {
+                const unsigned key = n * kRowsAtOnce + lane / kPieces;
+                const u64 vu = (u64)__shfl(safe, 16 * wave + key);
+                bring(A.v + vu * A.v_unit + (u64)((first + key) & mask) * A.token_bytes + head_off +
+                          16 * (lane % kPieces ^ turn(key)), lv + n * 1024);
+            }
+        }
+    }
+    __device__ void arrive(const AttendArgs&, u64 there, char* to) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (there == ~0ull) return;
+        // what is stored where no token is may be anything
+        for (unsigned i = threadIdx.x; i < 64 * kPieces; i += kWaves * 64)
+            if (!(there >> (i / kPieces) & 1))
+                *reinterpret_cast<u32x4*>(to + kKeyBytes + i * 16) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    __device__ u32x4 value(const char* from, int h, int c) const {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds4;
+        // this lane's row of the four that its quarter wave turns, and 8 bytes of it
+        const unsigned key = 32 * h + 4 * quad + col / 4, piece = 2 * c + (col % 4) / 2;
+        const char* at = from + kKeyBytes + key * (kDim * 2) + 16 * (piece ^ turn(key)) + 8 * (col % 2);
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)at);
+        // 16 keys on: turned alike
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at + 16 * kDim * 2));
+        const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
+        return u32x4{x[0], x[1], y[0], y[1]};
+    }
+    static constexpr __host__ __device__ unsigned column(unsigned quad, int r, int c) { return 16 * c + 4 * quad + r; }
+    __device__ f32x4 scales(const char*, unsigned, unsigned) const { return f32x4{1, 1, 1, 1}; }
+};
+
+// 64 kQ rows and a range of keys: each wave has 16 kQ rows and all keys, and a block of
+// 64 keys and values comes into LDS once for the four waves.  From about 150 rows on
+// the products bound it, below HBM does.
+template <class T, int kDim, bool kE4m3, int kQ, class Blocks>
+__device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds) {
+    typedef typename Keys<T, kDim, kE4m3>::P P;
+    constexpr int kCols = kDim / 16, kFrags = kDim / 32;
+    const unsigned lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const unsigned col = lane % 16, quad = lane / 16;
+    Blocks keys(A, lane, wave);
     const unsigned total = s.rows * A.per, tile = s.tile, split = s.split;
     const unsigned m0 = tile * 64 * kQ, mw = m0 + wave * 16 * kQ;   // the tile's, the wave's first row
     const unsigned last = min(total - 1, m0 + 64 * kQ - 1) / A.per;
@@ -779,54 +927,23 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
         return unit_of(A, own ? s.first[1] : s.first[0], (unsigned)(own ? b - range.nb0 : b) * kBlock + lane,
                        own ? range.most : s.keys[0]);
     };
-    K x;
-    auto load = [&](u64 b, int unit) {
-        const unsigned key0 = (unsigned)(b >= range.nb0 ? b - range.nb0 : b) * kBlock;
-        load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * wave, key0 + 16 * wave, x);
-    };
-    int unit = -1, next = -1;
+    auto key_of = [&](u64 b) { return (unsigned)(b >= range.nb0 ? b - range.nb0 : b) * kBlock; };
+    // units are looked up two blocks ahead of their use, keys asked for one ahead
+    int unit = -1, next = -1, after = -1;
     if (range.b0 < range.b1) {
         next = look_up(range.b0);
-        load(range.b0, next);
+        if (range.b0 + 1 < range.b1) after = look_up(range.b0 + 1);
+        keys.ask(A, head, next, key_of(range.b0), lds);
     }
     unsigned buffer = 0;
     for (u64 b = range.b0; b < range.b1; ++b, buffer ^= 1) {
         unit = next;
-        if (b + 1 < range.b1) next = look_up(b + 1);
+        next = after;
         const u64 there = __ballot(unit >= 0);
-        char* const lk = lds + buffer * kBuffer;
-        char* const lv = lk + kKeyBytes;
-        float* const ls = reinterpret_cast<float*>(lv + kValueBytes);
-        if (there != ~0ull) {
-            const unsigned bits = (unsigned)(there >> (16 * wave + 4 * quad)) & 15u;
-            clear_values(x, bits);
-            if constexpr (kE4m3) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (!(bits >> c & 1)) x.ks[c] = x.vs[c] = 0.f;
-            }
-        }
-#pragma unroll
-        for (int f = 0; f < kFrags; ++f) {
-            u32x4 kf = x.key(f);
-            if (A.dim != kDim && K::slot_dim(f, quad) >= A.dim) kf = u32x4{0, 0, 0, 0};
-            *reinterpret_cast<u32x4*>(lk + ((wave * kFrags + f) * 64 + lane) * 16) = kf;
-        }
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-            const unsigned sel = c % 2 ? 0x07060302u : 0x05040100u;
-            const u32x2 vf = {__builtin_amdgcn_perm(x.value(1, c / 2), x.value(0, c / 2), sel),
-                              __builtin_amdgcn_perm(x.value(3, c / 2), x.value(2, c / 2), sel)};
-            *reinterpret_cast<u32x2*>(lv + (((wave / 2) * kCols + c) * 64 + lane) * 16 + (wave % 2) * 8) = vf;
-        }
-        if constexpr (kE4m3) {
-            if (col == 0) {
-                *reinterpret_cast<f32x4*>(ls + 16 * wave + 4 * quad) = x.ks;
-                *reinterpret_cast<f32x4*>(ls + 64 + 16 * wave + 4 * quad) = x.vs;
-            }
-        }
-        __syncthreads();
-        if (b + 1 < range.b1) load(b + 1, next);
+        char* const lk = lds + buffer * Blocks::kBuffer;
+        keys.arrive(A, there, lk);
+        if (b + 1 < range.b1) keys.ask(A, head, next, key_of(b + 1), lds + (buffer ^ 1) * Blocks::kBuffer);
+        if (b + 2 < range.b1) after = look_up(b + 2);
         // scores
         f32x4 st[kQ][4];
 #pragma unroll
@@ -840,13 +957,13 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
                 for (int t = 0; t < kQ; ++t) st[t][j] = T::mma(kf, q[t][f], st[t][j]);
             }
             if constexpr (kE4m3) {
-                const f32x4 ks = *reinterpret_cast<const f32x4*>(ls + 16 * j + 4 * quad);
+                const f32x4 ks = keys.scales(lk, 0, 16 * j + 4 * quad);
 #pragma unroll
                 for (int t = 0; t < kQ; ++t) st[t][j] *= ks;
             }
         }
         const bool own = b >= range.nb0;
-        const unsigned key0 = (unsigned)(own ? b - range.nb0 : b) * kBlock;
+        const unsigned key0 = key_of(b);
         if (there != ~0ull || (own && key0 + kBlock > lim_all)) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -880,7 +997,7 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
                     e[c] = __builtin_amdgcn_exp2f(fmaf(st[t][j][c], scale, off));
                     soft[t].sum += e[c];
                 }
-                if constexpr (kE4m3) e *= *reinterpret_cast<const f32x4*>(ls + 64 + 16 * j + 4 * quad);
+                if constexpr (kE4m3) e *= keys.scales(lk, 1, 16 * j + 4 * quad);
                 w[t][j][0] = P::pack(e[0], e[1]);
                 w[t][j][1] = P::pack(e[2], e[3]);
             }
@@ -889,7 +1006,7 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-                const u32x4 vf = *reinterpret_cast<const u32x4*>(lv + ((h * kCols + c) * 64 + lane) * 16);
+                const u32x4 vf = keys.value(lk, h, c);
 #pragma unroll
                 for (int t = 0; t < kQ; ++t)
                     o[t][c] = P::mma(vf, u32x4{w[t][2 * h][0], w[t][2 * h][1], w[t][2 * h + 1][0],
@@ -909,19 +1026,22 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
         const unsigned row = m / A.per, hh = head * A.per + (m - row * A.per);
         const float mine = direct ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
         char* to = A.out + (u64)(s.row0 + row) * A.out_row + (u64)hh * A.out_head;
+        // four columns next to each other, of one product's rows or of four products
+        constexpr bool kByRow = Blocks::column(0, 1, 0) == 1;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const unsigned d = (4 * quad + r) * kCols;
-            if (d >= A.dim) continue;
+        for (int r = 0; r < (kByRow ? 1 : 4); ++r)
 #pragma unroll
-            for (int c = 0; c < kCols; c += 4) {
-                const f32x4 y = f32x4{o[t][c][r], o[t][c + 1][r], o[t][c + 2][r], o[t][c + 3][r]} * mine;
+            for (int c = 0; c < kCols; c += kByRow ? 1 : 4) {
+                const unsigned d = Blocks::column(quad, r, c);
+                if (d >= A.dim) continue;
+                const f32x4 y = (kByRow ? o[t][c] : f32x4{o[t][c][r], o[t][c + (kByRow ? 0 : 1)][r],
+                                                          o[t][c + (kByRow ? 0 : 2)][r],
+                                                          o[t][c + (kByRow ? 0 : 3)][r]}) * mine;
                 if (direct)
-                    *reinterpret_cast<u32x2*>(to + 2 * (d + c)) = u32x2{T::pack(y[0], y[1]), T::pack(y[2], y[3])};
+                    *reinterpret_cast<u32x2*>(to + 2 * d) = u32x2{T::pack(y[0], y[1]), T::pack(y[2], y[3])};
                 else
-                    *reinterpret_cast<f32x4*>(&A.part_o[(part0 + m) * kDim + d + c]) = y;
+                    *reinterpret_cast<f32x4*>(&A.part_o[(part0 + m) * kDim + d]) = y;
             }
-        }
         if (quad == 0) {
             if (direct) {
                 if (A.lse) A.lse[(u64)(s.row0 + row) * (A.n_heads * A.per) + hh] =
@@ -931,27 +1051,37 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
             }
         }
     }
-    __syncthreads();            // the next item's LDS
 }
 
-template <class T, int kDim, bool kE4m3, bool kWide>
+// kFull: a 16-bit cache whose dim is kDim.
+template <class T, int kDim, bool kE4m3, bool kWide, bool kFull>
 __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(AttendArgs A) {
     // two buffers of a block's keys, values and scales, or the waves' sums
     constexpr int kBlocks = 2 * (kDim * 256 + 512), kSums = kWaves * 16 * (kDim + 4) * 4 + kWaves * 16 * 8;
     __shared__ __align__(16) char lds[kBlocks > kSums ? kBlocks : kSums];
     __shared__ unsigned s_ticket[2];
     const u64 n = (u64)A.counts[0] * A.n_heads;
-    // Items are taken as workgroups get free.  Which workgroup computes an item
-    // changes nothing in its result.  The next one is asked for early.
+    // Items are taken as workgroups get free.  Which workgroup computes an item changes
+    // nothing in its result.  The next one is asked for early and looked at late.
     u64 it = blockIdx.x;
     for (unsigned turn = 0; it < n; turn ^= 1) {
-        if (threadIdx.x == 0) s_ticket[turn] = gridDim.x + atomicAdd(&A.counts[2], 1u);
+        unsigned ticket = 0;
+        if (threadIdx.x == 0) ticket = atomicAdd(A.taken, 1u);
         const unsigned head = (unsigned)(it % A.n_heads);
         const Item s = A.items[it / A.n_heads];
-        if (s.tile_rows == 16) few_rows<T, kDim, kE4m3, kWide>(A, s, head, lds);
-        else if (s.tile_rows == 64) many_rows<T, kDim, kE4m3, kWide, 1>(A, s, head, lds);
-        else many_rows<T, kDim, kE4m3, kWide, 2>(A, s, head, lds);
-        it = s_ticket[turn];
+        if (s.tile_rows == 16) {
+            few_rows<T, kDim, kE4m3, kWide>(A, s, head, lds);
+        } else if constexpr (kFull) {
+            if (s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Straight<T, kDim, kWide>>(A, s, head, lds);
+            else many_rows<T, kDim, kE4m3, 2, Straight<T, kDim, kWide>>(A, s, head, lds);
+        } else {
+            typedef ThroughRegisters<T, kDim, kE4m3, kWide> Blocks;
+            if (s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Blocks>(A, s, head, lds);
+            else many_rows<T, kDim, kE4m3, 2, Blocks>(A, s, head, lds);
+        }
+        if (threadIdx.x == 0) s_ticket[turn] = ticket;
+        __syncthreads();
+        it = (u64)gridDim.x + s_ticket[turn];
     }
 }
 
@@ -1088,9 +1218,12 @@ Layout layout_of(u64 n_rows, u64 n_requests, u64 n_groups, u64 n_heads, u64 per,
 template <class T, int kDim, bool kE4m3>
 void attend_launch(const AttendArgs& A, unsigned cus, hipStream_t st) {
     hipLaunchKernelGGL(k_attend_plan, dim3(1), dim3(kPlanThreads), 0, st, A);
-    const dim3 grid(cus * (kDim > 128 ? 1 : 2)), block(kWaves * 64);
-    if (A.shift >= 4) hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, true>), grid, block, 0, st, A);
-    else hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, false>), grid, block, 0, st, A);
+    const dim3 grid((cus * (kDim > 128 ? 1 : 2) + kXcds - 1) / kXcds * kXcds), block(kWaves * 64);
+    const bool wide = A.shift >= 4, full = !kE4m3 && A.dim == kDim;
+    if (full && wide) hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, true, !kE4m3>), grid, block, 0, st, A);
+    else if (full) hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, false, !kE4m3>), grid, block, 0, st, A);
+    else if (wide) hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, true, false>), grid, block, 0, st, A);
+    else hipLaunchKernelGGL((k_attend<T, kDim, kE4m3, false, false>), grid, block, 0, st, A);
     const u64 rows = (u64)A.n_rows * A.n_heads * A.per;
     hipLaunchKernelGGL((k_attend_join<T, kDim>), dim3((unsigned)std::min<u64>(rows, 8 * cus)), dim3(256), 0,
                        st, A);
@@ -1205,6 +1338,7 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     A.q_flip = scale < 0.f ? 0x80008000u : 0u;
     char* ws = static_cast<char*>(workspace);
     A.counts = reinterpret_cast<unsigned*>(ws);
+    A.taken = A.counts + 8;
     A.items = reinterpret_cast<Item*>(ws + l.items);
     A.joins = reinterpret_cast<JoinRow*>(ws + l.joins);
     A.most_items = most_items(rows, batch->n_requests + batch->n_groups, n_q_heads / cache->n_heads);

