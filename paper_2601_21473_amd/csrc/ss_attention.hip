@@ -151,16 +151,18 @@ __device__ Stack request_stack(const AttendArgs& A, unsigned s) {
     return t;
 }
 
-// Adds request s's prefix, if its group has one: as keys of its own or as a pool.
-__device__ void add_prefix(const AttendArgs& A, unsigned s, Stack& t) {
-    unsigned lo = 0, hi = A.n_groups;           // the largest g with group_off[g] <= s
+// Adds to request s's stack its group's prefix, as keys of its own or as a pool.  begin
+// and end are the groups' offsets, prefix their stacks.
+template <class P, class B>
+__device__ void add_prefix(unsigned s, unsigned n_groups, B begin, const P& prefix, Stack& t) {
+    unsigned lo = 0, hi = n_groups;             // the largest g with begin(g) <= s
     while (hi - lo > 1) {
         const unsigned mid = (lo + hi) / 2;
-        if (A.group_off[mid] <= s) lo = mid;
+        if (begin(mid) <= s) lo = mid;
         else hi = mid;
     }
-    if (hi <= lo || A.group_off[lo] > s || s >= A.group_off[lo + 1]) return;
-    const Stack& p = A.stacks[lo];
+    if (hi <= lo || begin(lo) > s || s >= begin(lo + 1)) return;
+    const Stack& p = prefix[lo];
     if (p.rows) {
         t.pool = lo;
     } else {
@@ -177,9 +179,10 @@ struct PlanState {
     unsigned base[3];                           // items, rows to join, parts per head so far
 };
 
-// Lists the items and the rows to join of up to kPlanThreads stacks, thread by thread.
+// Lists the items and the rows to join of up to kPlanThreads stacks, thread by thread;
+// pools are in `prefix`, where a prefix's own stack (`group`) goes too.
 __device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned group, unsigned chunk,
-                            PlanState& S) {
+                            Stack* prefix, bool more, PlanState& S) {
     const unsigned tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const unsigned blocks = blocks_of(t);
     t.splits = blocks / chunk + (blocks % chunk != 0);
@@ -208,7 +211,7 @@ __device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned gro
         for (unsigned w = 0; w < wave; ++w) a[k] += S.sum[w][k];
     }
     if (v[2]) t.part = (u64)(S.base[2] + a[2]) * A.n_heads;
-    if (group != kNone) A.stacks[group] = t;
+    if (group != kNone) prefix[group] = t;
     S.stack[tid] = t;
     S.at[0][tid] = a[0];
     S.at[1][tid] = a[1];
@@ -226,17 +229,19 @@ __device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned gro
         return lo;
     };
     const unsigned items = S.at[0][kPlanThreads], joins = S.at[1][kPlanThreads];
-    if ((u64)S.base[0] + items <= A.most_items)
+    const unsigned base0 = S.base[0], base1 = S.base[1];
+    if (!more) __syncthreads();
+    if ((u64)base0 + items <= A.most_items)
         for (unsigned i = tid; i < items; i += kPlanThreads) {
             const unsigned f = find(0, i), j = i - S.at[0][f];
             const Stack& s = S.stack[f];
             const unsigned tiles = tiles_of(A, s);
             // tiles next to each other read the same keys
-            A.items[S.base[0] + i] = Item{{s.first[0], s.first[1]}, s.part, {s.keys[0], s.keys[1]},
+            A.items[base0 + i] = Item{{s.first[0], s.first[1]}, s.part, {s.keys[0], s.keys[1]},
                                           s.row0, s.rows, s.see, s.splits, tile_rows(A, s),
                                           j % tiles, j / tiles, chunk};
         }
-    if ((u64)S.base[1] + joins <= A.n_rows)
+    if ((u64)base1 + joins <= A.n_rows)
         for (unsigned i = tid; i < joins; i += kPlanThreads) {
             const unsigned f = find(1, i);
             const Stack& s = S.stack[f];
@@ -246,7 +251,7 @@ __device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned gro
             r.total[0] = s.rows * A.per;
             r.splits[0] = s.splits;
             if (s.pool != kNone) {
-                const Stack& p = A.stacks[s.pool];
+                const Stack& p = prefix[s.pool];
                 // offsets that break the rules can put a request outside its group's rows
                 if (r.row >= p.row0 && r.row - p.row0 < p.rows) {
                     r.first[1] = p.part + (u64)(r.row - p.row0) * A.per;
@@ -254,15 +259,15 @@ __device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned gro
                     r.splits[1] = p.splits;
                 }
             }
-            A.joins[S.base[1] + i] = r;
+            A.joins[base1 + i] = r;
         }
-    __syncthreads();
+    if (more) __syncthreads();          // before base changes
     if (tid == kPlanThreads - 1) {
         S.base[0] += a[0] + v[0];
         S.base[1] += a[1] + v[1];
         S.base[2] += a[2] + v[2];
     }
-    __syncthreads();
+    if (more) __syncthreads();
 }
 
 // One workgroup: the stacks, how they are split, and what there is to do.  Keys are cut
@@ -278,21 +283,43 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
     float work = 0.f;
     unsigned own_rows = 0, pool_rows = 0;       // saturating: one of n_rows says enough
     auto add = [](unsigned a, unsigned b) { return a + b < a ? ~0u : a + b; };
+    // Batches of up to kPlanThreads requests and groups: groups in the first threads,
+    // requests in the last, so that they are in other waves as a rule and read at the
+    // same time; all in LDS.  Larger ones: groups in the workspace, requests one thousand
+    // after the other, and again for their items.
+    const unsigned n_requests = A.n_requests, n_groups = A.n_groups;
+    const bool small = n_requests + n_groups <= kPlanThreads;
+    const bool is_group = tid < n_groups, is_request = kPlanThreads - 1 - tid < n_requests;
     Stack mine{};
-    if (tid < A.n_requests) mine = request_stack(A, tid);
-    for (unsigned g = tid; g < A.n_groups; g += kPlanThreads) {
-        const Stack t = prefix_stack(A, g);
-        A.stacks[g] = t;
-        work += (float)tiles_of(A, t) * (float)blocks_of(t);
-        pool_rows = add(pool_rows, t.rows);
-    }
-    __syncthreads();
-    for (unsigned s = tid; s < A.n_requests; s += kPlanThreads) {
-        Stack t = s < kPlanThreads ? mine : request_stack(A, s);
-        if (A.n_groups) add_prefix(A, s, t);
-        if (s < kPlanThreads) mine = t;
-        work += (float)tiles_of(A, t) * (float)blocks_of(t);
-        own_rows = add(own_rows, t.rows);
+    if (small) {
+        if (is_group) {
+            mine = prefix_stack(A, tid);
+            S.stack[tid] = mine;
+            S.at[0][tid] = A.group_off[tid];
+            if (tid == n_groups - 1) S.at[0][n_groups] = A.group_off[n_groups];
+            pool_rows = mine.rows;
+        } else if (is_request) {
+            mine = request_stack(A, kPlanThreads - 1 - tid);
+            own_rows = mine.rows;
+        }
+        __syncthreads();
+        if (is_request && n_groups)
+            add_prefix(kPlanThreads - 1 - tid, n_groups, [&](unsigned g) { return S.at[0][g]; }, S.stack, mine);
+        work = (float)tiles_of(A, mine) * (float)blocks_of(mine);
+    } else {
+        for (unsigned g = tid; g < n_groups; g += kPlanThreads) {
+            const Stack t = prefix_stack(A, g);
+            A.stacks[g] = t;
+            work += (float)tiles_of(A, t) * (float)blocks_of(t);
+            pool_rows = add(pool_rows, t.rows);
+        }
+        __syncthreads();
+        for (unsigned s = tid; s < n_requests; s += kPlanThreads) {
+            Stack t = request_stack(A, s);
+            add_prefix(s, n_groups, [&](unsigned g) { return A.group_off[g]; }, A.stacks, t);
+            work += (float)tiles_of(A, t) * (float)blocks_of(t);
+            own_rows = add(own_rows, t.rows);
+        }
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) {
@@ -320,21 +347,26 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
     // offsets that give a row to two requests: nothing is computed
     if (own_rows <= A.n_rows && pool_rows <= A.n_rows) {
         // prefixes first: their items are the longest
-        for (unsigned g0 = 0; g0 < A.n_groups; g0 += kPlanThreads) {
-            const unsigned g = g0 + tid;
-            plan_stacks(A, g < A.n_groups ? A.stacks[g] : Stack{}, false, g < A.n_groups ? g : kNone,
-                        chunk, S);
-        }
-        for (unsigned s0 = 0; s0 < A.n_requests; s0 += kPlanThreads) {
-            const unsigned s = s0 + tid;
-            Stack t{};
-            if (s < A.n_requests) {
-                t = s0 ? request_stack(A, s) : mine;
-                if (s0 && A.n_groups) add_prefix(A, s, t);
+        if (small) {
+            plan_stacks(A, mine, is_request, is_group ? tid : kNone, chunk, S.stack, false, S);
+        } else {
+            for (unsigned g0 = 0; g0 < n_groups; g0 += kPlanThreads) {
+                const unsigned g = g0 + tid;
+                plan_stacks(A, g < n_groups ? A.stacks[g] : Stack{}, false, g < n_groups ? g : kNone,
+                            chunk, A.stacks, true, S);
             }
-            plan_stacks(A, t, s < A.n_requests, kNone, chunk, S);
+            for (unsigned s0 = 0; s0 < n_requests; s0 += kPlanThreads) {
+                const unsigned s = s0 + tid;
+                Stack t{};
+                if (s < n_requests) {
+                    t = request_stack(A, s);
+                    add_prefix(s, n_groups, [&](unsigned g) { return A.group_off[g]; }, A.stacks, t);
+                }
+                plan_stacks(A, t, s < n_requests, kNone, chunk, A.stacks, true, S);
+            }
         }
     }
+    __syncthreads();
     if (tid == 0) {
         // more than the workspace holds cannot be for valid offsets
         const bool fits = (u64)S.base[2] * A.n_heads <= A.part_rows && S.base[0] <= A.most_items &&
@@ -499,12 +531,12 @@ __device__ __forceinline__ int unit_of(const AttendArgs& A, u64 first, unsigned 
 // blocks, of which the tile's rows see own tokens below `most`.
 struct Range {
     unsigned nb0, most;
-    u64 b0, b1;
+    unsigned b0, b1;            // below 2^28 + chunk
     __device__ Range(const AttendArgs& A, const Item& s, unsigned last_row, unsigned split) {
         most = (unsigned)min((long long)s.keys[1], max(0ll, (long long)s.see + last_row + 1));
         nb0 = (s.keys[0] + kBlock - 1) / kBlock;
-        b0 = (u64)split * s.chunk;
-        b1 = min((u64)nb0 + (most + kBlock - 1) / kBlock, b0 + s.chunk);
+        b0 = split * s.chunk;
+        b1 = min(nb0 + (most + kBlock - 1) / kBlock, b0 + s.chunk);
     }
 };
 
@@ -585,15 +617,15 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
     for (int i = 0; i < kCols; ++i) o[i] = f32x4{0, 0, 0, 0};
     Softmax soft;
 
-    const u64 blocks = range.b1 > range.b0 + wave ? (range.b1 - range.b0 - wave + kWaves - 1) / kWaves : 0;
-    const u64 steps = blocks * kSteps;
+    const unsigned blocks = range.b1 > range.b0 + wave ? (range.b1 - range.b0 - wave + kWaves - 1) / kWaves : 0;
+    const unsigned steps = blocks * kSteps;
     // step i: its segment's first entry, first key, number of keys
-    auto where = [&](u64 i, bool* own, unsigned* key0) {
-        const u64 b = range.b0 + wave + i / kSteps * kWaves;
+    auto where = [&](unsigned i, bool* own, unsigned* key0) {
+        const unsigned b = range.b0 + wave + i / kSteps * kWaves;
         *own = b >= range.nb0;
-        *key0 = (unsigned)(*own ? b - range.nb0 : b) * kBlock + (unsigned)(i % kSteps) * (16 * kSub);
+        *key0 = (*own ? b - range.nb0 : b) * kBlock + i % kSteps * (16 * kSub);
     };
-    auto look_up = [&](u64 i) {
+    auto look_up = [&](unsigned i) {
         bool own;
         unsigned key0;
         where(i, &own, &key0);
@@ -604,7 +636,7 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
         K x[kSub];
         u64 there;
     };
-    auto load = [&](u64 i, int unit, Step& t) {
+    auto load = [&](unsigned i, int unit, Step& t) {
         bool own;
         unsigned key0;
         where(i, &own, &key0);
@@ -613,7 +645,7 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
         for (int j = 0; j < kSub; ++j)
             load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * j, key0 + 16 * j, t.x[j]);
     };
-    auto compute = [&](u64 i, Step& t) {
+    auto compute = [&](unsigned i, Step& t) {
         bool own;
         unsigned key0;
         where(i, &own, &key0);
@@ -681,19 +713,34 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
             }
         }
     };
-    if (steps) {
+    // units are looked up two steps ahead of their use, keys asked for one ahead
+    // (where 64 KB of registers hold two steps)
+    if constexpr (kDim <= 128 || kE4m3) {
         Step a, b;
-        int unit = look_up(0);
-        load(0, unit, a);
-        unit = steps > 1 ? look_up(1) : -1;
-        for (u64 i = 0; i < steps; i += 2) {
-            if (i + 1 < steps) load(i + 1, unit, b);
-            if (i + 2 < steps) unit = look_up(i + 2);
+        int next = -1, after = -1;
+        if (steps > 0) next = look_up(0);
+        if (steps > 1) after = look_up(1);
+        if (steps > 0) load(0, next, a);
+        for (unsigned i = 0; i < steps; i += 2) {
+            next = after;
+            if (i + 2 < steps) after = look_up(i + 2);
+            if (i + 1 < steps) load(i + 1, next, b);
             compute(i, a);
             if (i + 1 >= steps) break;
-            if (i + 2 < steps) load(i + 2, unit, a);
-            if (i + 3 < steps) unit = look_up(i + 3);
+            next = after;
+            if (i + 3 < steps) after = look_up(i + 3);
+            if (i + 2 < steps) load(i + 2, next, a);
             compute(i + 1, b);
+        }
+    } else {
+        int next = -1;
+        if (steps > 0) next = look_up(0);
+        for (unsigned i = 0; i < steps; ++i) {
+            const int unit = next;
+            if (i + 1 < steps) next = look_up(i + 1);
+            Step a;
+            load(i, unit, a);
+            compute(i, a);
         }
     }
     float sum = soft.sum;
@@ -922,12 +969,12 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
     const unsigned lim_all = (unsigned)min((long long)s.keys[1],
                                            max(0ll, (long long)s.see + mw / A.per + 1));
     const float scale = A.scale;
-    auto look_up = [&](u64 b) {
+    auto look_up = [&](unsigned b) {
         const bool own = b >= range.nb0;
-        return unit_of(A, own ? s.first[1] : s.first[0], (unsigned)(own ? b - range.nb0 : b) * kBlock + lane,
+        return unit_of(A, own ? s.first[1] : s.first[0], (own ? b - range.nb0 : b) * kBlock + lane,
                        own ? range.most : s.keys[0]);
     };
-    auto key_of = [&](u64 b) { return (unsigned)(b >= range.nb0 ? b - range.nb0 : b) * kBlock; };
+    auto key_of = [&](unsigned b) { return (b >= range.nb0 ? b - range.nb0 : b) * kBlock; };
     // units are looked up two blocks ahead of their use, keys asked for one ahead
     int unit = -1, next = -1, after = -1;
     if (range.b0 < range.b1) {
@@ -936,7 +983,7 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
         keys.ask(A, head, next, key_of(range.b0), lds);
     }
     unsigned buffer = 0;
-    for (u64 b = range.b0; b < range.b1; ++b, buffer ^= 1) {
+    for (unsigned b = range.b0; b < range.b1; ++b, buffer ^= 1) {
         unit = next;
         next = after;
         const u64 there = __ballot(unit >= 0);
@@ -1060,14 +1107,16 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
     constexpr int kBlocks = 2 * (kDim * 256 + 512), kSums = kWaves * 16 * (kDim + 4) * 4 + kWaves * 16 * 8;
     __shared__ __align__(16) char lds[kBlocks > kSums ? kBlocks : kSums];
     __shared__ unsigned s_ticket[2];
-    const u64 n = (u64)A.counts[0] * A.n_heads;
+    const unsigned n = A.counts[0] * A.n_heads;
     // Items are taken as workgroups get free.  Which workgroup computes an item changes
-    // nothing in its result.  The next one is asked for early and looked at late.
-    u64 it = blockIdx.x;
+    // nothing in its result.  The next number is asked for early and looked at late; asked
+    // for two ahead, with the item read one ahead, workgroups hold items that others
+    // could take (64 agents over 8,192 tokens 84 us, as it is 70 us).
+    unsigned it = blockIdx.x;
     for (unsigned turn = 0; it < n; turn ^= 1) {
         unsigned ticket = 0;
         if (threadIdx.x == 0) ticket = atomicAdd(A.taken, 1u);
-        const unsigned head = (unsigned)(it % A.n_heads);
+        const unsigned head = it % A.n_heads;
         const Item s = A.items[it / A.n_heads];
         if (s.tile_rows == 16) {
             few_rows<T, kDim, kE4m3, kWide>(A, s, head, lds);
@@ -1081,7 +1130,7 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
         }
         if (threadIdx.x == 0) s_ticket[turn] = ticket;
         __syncthreads();
-        it = (u64)gridDim.x + s_ticket[turn];
+        it = gridDim.x + s_ticket[turn];
     }
 }
 
@@ -1091,12 +1140,12 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
 // caches), so the parts are read along with their references, eight at a time, and
 // small batches get a workgroup a row (one wave took 81 us for 128 parts of 32 rows).
 template <class T, int kDim, int kTeam>
-__device__ __forceinline__ void join_row(const AttendArgs& A, u64 w, float (*s_x)[kDim], float2* s_ml) {
+__device__ __forceinline__ void join_row(const AttendArgs& A, unsigned w, float (*s_x)[kDim], float2* s_ml) {
     constexpr int kCols = kDim / 64;
     const unsigned lane = threadIdx.x % 64, member = kTeam == 1 ? 0 : threadIdx.x / 64;
     const unsigned heads = A.n_heads * A.per;
     const JoinRow r = A.joins[w / heads];
-    const unsigned qh = (unsigned)(w % heads), head = qh / A.per, g = qh - head * A.per;
+    const unsigned qh = w % heads, head = qh / A.per, g = qh - head * A.per;
     const u64 first0 = r.first[0] + (u64)head * r.splits[0] * r.total[0] + g;
     const u64 first1 = r.first[1] + (u64)head * r.splits[1] * r.total[1] + g;
     const unsigned parts = r.splits[0] + r.splits[1];
@@ -1177,11 +1226,11 @@ template <class T, int kDim>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs A) {
     __shared__ float s_x[4][kDim];
     __shared__ float2 s_ml[4];
-    const u64 n = (u64)A.counts[1] * (A.n_heads * A.per);
+    const unsigned n = A.counts[1] * (A.n_heads * A.per);      // below 2^30
     if (n <= gridDim.x) {
         if (blockIdx.x < n) join_row<T, kDim, 4>(A, blockIdx.x, s_x, s_ml);
     } else {
-        for (u64 w = blockIdx.x * 4 + threadIdx.x / 64; w < n; w += gridDim.x * 4)
+        for (unsigned w = blockIdx.x * 4 + threadIdx.x / 64; w < n; w += gridDim.x * 4)
             join_row<T, kDim, 1>(A, w, s_x, s_ml);
     }
 }
@@ -1246,6 +1295,9 @@ ss_status attend_args(const ss_kv_cache* c, const ss_batch* b, uint32_t type, ui
         return set_err(SS_ERR_ARG, "n_q_heads must be a multiple of the cache's n_heads, at most 65536");
     if ((u64)b->n_rows * n_q_heads >= (1ull << 30))
         return set_err(SS_ERR_ARG, "n_rows * n_q_heads must be below 2^30");
+    const u64 n_stacks = (u64)b->n_requests + b->n_groups;
+    if (most_items(b->n_rows, n_stacks, n_q_heads / c->n_heads) * c->n_heads >= (1ull << 31))
+        return set_err(SS_ERR_ARG, "(n_requests + n_groups) * n_heads is too large");
     return SS_OK;
 }
 
