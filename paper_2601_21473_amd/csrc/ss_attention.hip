@@ -102,10 +102,10 @@ __device__ unsigned blocks_of(const Stack& s) {
     return (s.keys[0] + kBlock - 1) / kBlock + (s.keys[1] + kBlock - 1) / kBlock;
 }
 // Rows of a stack's tiles: 16 while they hold all (nothing to share, so registers
-// suffice), else 64 or 128 through LDS.
+// suffice), else 64 or, where the registers hold the sums of so many, 128 through LDS.
 __device__ unsigned tile_rows(const AttendArgs& A, const Stack& s) {
     const u64 rows = (u64)s.rows * A.per;
-    return rows <= 16 ? 16 : rows <= 64 ? 64 : 128;
+    return rows <= 16 ? 16 : rows <= 64 || A.dim > 128 ? 64 : 128;
 }
 __device__ unsigned tiles_of(const AttendArgs& A, const Stack& s) {
     const u64 n = tile_rows(A, s);
@@ -522,9 +522,13 @@ __device__ __forceinline__ void clear_values(K& x, unsigned there) {
         }
 }
 
-// The unit of key `key` of a segment, -1 where there is none.
-__device__ __forceinline__ int unit_of(const AttendArgs& A, u64 first, unsigned key, unsigned limit) {
-    return key < limit ? A.tab.unit(first + (key >> A.shift)) : -1;
+// The table's entry for key `key` of a segment, -1 where there is none, as it is read:
+// whether it is a unit is asked when it is used, or the read would be waited for.
+__device__ __forceinline__ int entry_of(const AttendArgs& A, u64 first, unsigned key, unsigned limit) {
+    return key < limit ? A.tab.units[first + (key >> A.shift)] : -1;
+}
+__device__ __forceinline__ int unit_of(const AttendArgs& A, int entry) {
+    return entry >= 0 && (u64)entry < A.tab.capacity ? entry : -1;
 }
 
 // The keys that an item reads: blocks [b0, b1) of the prefix's and the own tokens'
@@ -629,14 +633,15 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
         bool own;
         unsigned key0;
         where(i, &own, &key0);
-        return unit_of(A, own ? s.first[1] : s.first[0], key0 + lane % (16 * kSub),
+        return entry_of(A, own ? s.first[1] : s.first[0], key0 + lane % (16 * kSub),
                        own ? range.most : s.keys[0]);
     };
     struct Step {
         K x[kSub];
         u64 there;
     };
-    auto load = [&](unsigned i, int unit, Step& t) {
+    auto load = [&](unsigned i, int entry, Step& t) {
+        const int unit = unit_of(A, entry);
         bool own;
         unsigned key0;
         where(i, &own, &key0);
@@ -736,10 +741,10 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
         int next = -1;
         if (steps > 0) next = look_up(0);
         for (unsigned i = 0; i < steps; ++i) {
-            const int unit = next;
+            const int entry = next;
             if (i + 1 < steps) next = look_up(i + 1);
             Step a;
-            load(i, unit, a);
+            load(i, entry, a);
             compute(i, a);
         }
     }
@@ -848,6 +853,10 @@ struct ThroughRegisters {
         }
         __syncthreads();
     }
+    // Fragment i of the keys, 16 of them for each kFrags.
+    __device__ u32x4 key(const char* from, int i) const {
+        return *reinterpret_cast<const u32x4*>(from + (i * 64 + lane) * 16);
+    }
     // Fragment c of the values of keys 32 h ..; row r of a lane's product is the column:
     __device__ u32x4 value(const char* from, int h, int c) const {
         return *reinterpret_cast<const u32x4*>(from + kKeyBytes + ((h * kCols + c) * 64 + lane) * 16);
@@ -923,6 +932,9 @@ struct Straight {
                 *reinterpret_cast<u32x4*>(to + kKeyBytes + i * 16) = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
+    __device__ u32x4 key(const char* from, int i) const {
+        return *reinterpret_cast<const u32x4*>(from + (i * 64 + lane) * 16);
+    }
     __device__ u32x4 value(const char* from, int h, int c) const {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 lds4;
@@ -943,7 +955,7 @@ struct Straight {
 // 64 keys and values comes into LDS once for the four waves.  From about 150 rows on
 // the products bound it, below HBM does.
 template <class T, int kDim, bool kE4m3, int kQ, class Blocks>
-__device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds) {
+__device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds0, char* lds1) {
     typedef typename Keys<T, kDim, kE4m3>::P P;
     constexpr int kCols = kDim / 16, kFrags = kDim / 32;
     const unsigned lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -971,44 +983,60 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
     const float scale = A.scale;
     auto look_up = [&](unsigned b) {
         const bool own = b >= range.nb0;
-        return unit_of(A, own ? s.first[1] : s.first[0], (own ? b - range.nb0 : b) * kBlock + lane,
+        return entry_of(A, own ? s.first[1] : s.first[0], (own ? b - range.nb0 : b) * kBlock + lane,
                        own ? range.most : s.keys[0]);
     };
     auto key_of = [&](unsigned b) { return (b >= range.nb0 ? b - range.nb0 : b) * kBlock; };
     // units are looked up two blocks ahead of their use, keys asked for one ahead
-    int unit = -1, next = -1, after = -1;
+    int next = -1, after = -1;
     if (range.b0 < range.b1) {
         next = look_up(range.b0);
         if (range.b0 + 1 < range.b1) after = look_up(range.b0 + 1);
-        keys.ask(A, head, next, key_of(range.b0), lds);
+        keys.ask(A, head, unit_of(A, next), key_of(range.b0), lds0);
     }
-    unsigned buffer = 0;
-    for (unsigned b = range.b0; b < range.b1; ++b, buffer ^= 1) {
-        unit = next;
+    // One block, in buffer `here`, while the next one comes into `there`.  The products'
+    // fragments are read a group ahead of their use: an LDS read takes about as long as
+    // eight products, and the compiler by itself waits for each (16 prompts 989 us).
+    auto block = [&](unsigned b, char* __restrict__ here, char* __restrict__ beside) {
+        const u64 there = __ballot(unit_of(A, next) >= 0);
         next = after;
-        const u64 there = __ballot(unit >= 0);
-        char* const lk = lds + buffer * Blocks::kBuffer;
-        keys.arrive(A, there, lk);
-        if (b + 1 < range.b1) keys.ask(A, head, next, key_of(b + 1), lds + (buffer ^ 1) * Blocks::kBuffer);
+        keys.arrive(A, there, here);
+        if (b + 1 < range.b1) keys.ask(A, head, unit_of(A, next), key_of(b + 1), beside);
         if (b + 2 < range.b1) after = look_up(b + 2);
         // scores
         f32x4 st[kQ][4];
+        u32x4 kf[2][kFrags];
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) kf[0][f] = keys.key(here, f);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            if (j < 3) {
+#pragma unroll
+                for (int f = 0; f < kFrags; ++f) kf[(j + 1) % 2][f] = keys.key(here, (j + 1) * kFrags + f);
+            }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int t = 0; t < kQ; ++t) st[t][j] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int f = 0; f < kFrags; ++f) {
-                const u32x4 kf = *reinterpret_cast<const u32x4*>(lk + ((j * kFrags + f) * 64 + lane) * 16);
+            for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-                for (int t = 0; t < kQ; ++t) st[t][j] = T::mma(kf, q[t][f], st[t][j]);
-            }
-            if constexpr (kE4m3) {
-                const f32x4 ks = keys.scales(lk, 0, 16 * j + 4 * quad);
+                for (int t = 0; t < kQ; ++t) st[t][j] = T::mma(kf[j % 2][f], q[t][f], st[t][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (kE4m3) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 ks = keys.scales(here, 0, 16 * j + 4 * quad);
 #pragma unroll
                 for (int t = 0; t < kQ; ++t) st[t][j] *= ks;
             }
         }
+        // values in groups of kGroup columns' fragments, the first one while the
+        // weights are worked out
+        constexpr int kGroup = 4, kGroups = 2 * kCols / kGroup;
+        u32x4 vf[2][kGroup];
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g) vf[0][g] = keys.value(here, 0, g);
         const bool own = b >= range.nb0;
         const unsigned key0 = key_of(b);
         if (there != ~0ull || (own && key0 + kBlock > lim_all)) {
@@ -1044,21 +1072,32 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
                     e[c] = __builtin_amdgcn_exp2f(fmaf(st[t][j][c], scale, off));
                     soft[t].sum += e[c];
                 }
-                if constexpr (kE4m3) e *= keys.scales(lk, 1, 16 * j + 4 * quad);
+                if constexpr (kE4m3) e *= keys.scales(here, 1, 16 * j + 4 * quad);
                 w[t][j][0] = P::pack(e[0], e[1]);
                 w[t][j][1] = P::pack(e[2], e[3]);
             }
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < kGroups; ++i) {
+            if (i + 1 < kGroups) {
 #pragma unroll
-            for (int c = 0; c < kCols; ++c) {
-                const u32x4 vf = keys.value(lk, h, c);
+                for (int g = 0; g < kGroup; ++g)
+                    vf[(i + 1) % 2][g] = keys.value(here, (i + 1) * kGroup / kCols, (i + 1) * kGroup % kCols + g);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            const int h = i * kGroup / kCols, c = i * kGroup % kCols;
+#pragma unroll
+            for (int g = 0; g < kGroup; ++g)
 #pragma unroll
                 for (int t = 0; t < kQ; ++t)
-                    o[t][c] = P::mma(vf, u32x4{w[t][2 * h][0], w[t][2 * h][1], w[t][2 * h + 1][0],
-                                               w[t][2 * h + 1][1]}, o[t][c]);
-            }
+                    o[t][c + g] = P::mma(vf[i % 2][g], u32x4{w[t][2 * h][0], w[t][2 * h][1], w[t][2 * h + 1][0],
+                                                             w[t][2 * h + 1][1]}, o[t][c + g]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    for (unsigned b = range.b0; b < range.b1; b += 2) {
+        block(b, lds0, lds1);
+        if (b + 1 < range.b1) block(b + 1, lds1, lds0);
     }
     const bool direct = s.part == ~0ull;
     const u64 part0 = s.part + ((u64)head * s.splits + split) * total;
@@ -1103,9 +1142,11 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
 // kFull: a 16-bit cache whose dim is kDim.
 template <class T, int kDim, bool kE4m3, bool kWide, bool kFull>
 __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(AttendArgs A) {
-    // two buffers of a block's keys, values and scales, or the waves' sums
-    constexpr int kBlocks = 2 * (kDim * 256 + 512), kSums = kWaves * 16 * (kDim + 4) * 4 + kWaves * 16 * 8;
+    // two buffers of a block's keys, values and scales, or the waves' sums; two arrays,
+    // so that reads of the one do not wait for what comes into the other
+    constexpr int kBlocks = kDim * 256 + 512, kSums = kWaves * 16 * (kDim + 4) * 4 + kWaves * 16 * 8;
     __shared__ __align__(16) char lds[kBlocks > kSums ? kBlocks : kSums];
+    __shared__ __align__(16) char lds1[kBlocks];
     __shared__ unsigned s_ticket[2];
     const unsigned n = A.counts[0] * A.n_heads;
     // Items are taken as workgroups get free.  Which workgroup computes an item changes
@@ -1120,13 +1161,11 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
         const Item s = A.items[it / A.n_heads];
         if (s.tile_rows == 16) {
             few_rows<T, kDim, kE4m3, kWide>(A, s, head, lds);
-        } else if constexpr (kFull) {
-            if (s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Straight<T, kDim, kWide>>(A, s, head, lds);
-            else many_rows<T, kDim, kE4m3, 2, Straight<T, kDim, kWide>>(A, s, head, lds);
         } else {
-            typedef ThroughRegisters<T, kDim, kE4m3, kWide> Blocks;
-            if (s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Blocks>(A, s, head, lds);
-            else many_rows<T, kDim, kE4m3, 2, Blocks>(A, s, head, lds);
+            typedef typename std::conditional<kFull, Straight<T, kDim, kWide>,
+                                              ThroughRegisters<T, kDim, kE4m3, kWide>>::type Blocks;
+            if (kDim > 128 || s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Blocks>(A, s, head, lds, lds1);
+            else if constexpr (kDim <= 128) many_rows<T, kDim, kE4m3, 2, Blocks>(A, s, head, lds, lds1);
         }
         if (threadIdx.x == 0) s_ticket[turn] = ticket;
         __syncthreads();
