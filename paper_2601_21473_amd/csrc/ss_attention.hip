@@ -941,9 +941,11 @@ struct Straight {
         // this lane's row of the four that its quarter wave turns, and 8 bytes of it
         const unsigned key = 32 * h + 4 * quad + col / 4, piece = 2 * c + (col % 4) / 2;
         const char* at = from + kKeyBytes + key * (kDim * 2) + 16 * (piece ^ turn(key)) + 8 * (col % 2);
+        // 16 keys on, turned alike; written out, as the compiler else takes it for the buffer
+        // that the next block comes into and waits for that (16 prompts 776 us)
+        const char* at2 = from + kKeyBytes + (key + 16) * (kDim * 2) + 16 * (piece ^ turn(key)) + 8 * (col % 2);
         const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)at);
-        // 16 keys on: turned alike
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(at + 16 * kDim * 2));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)at2);
         const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
         return u32x4{x[0], x[1], y[0], y[1]};
     }
