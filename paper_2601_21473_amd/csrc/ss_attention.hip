@@ -81,7 +81,7 @@ struct AttendArgs {
     unsigned q_keep, q_flip;                    // queries' bits that count, and that turn
     // workspace
     unsigned* counts;                           // items per head, rows to join
-    unsigned* taken;                            // [kXcds] items taken behind the first
+    unsigned* taken;                            // [16 kXcds] items taken behind the first
     Item* items;                                // [most_items]
     JoinRow* joins;                             // [n_rows]
     Stack* stacks;                              // [n_groups] of the prefixes
@@ -374,7 +374,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
         A.counts[0] = fits ? S.base[0] : 0;
         A.counts[1] = fits ? S.base[1] : 0;
     }
-    if (tid < kXcds) A.taken[tid] = 0;
+    if (tid < kXcds) A.taken[16 * tid] = 0;
 }
 
 constexpr int kWaves = 4;
@@ -382,6 +382,15 @@ constexpr int kWaves = 4;
 // the reference then stays for most blocks, and a block's maximum need not be known
 // to all lanes of a row.  2^8 is exact in every type and far from their ranges.
 constexpr float kSlack = 8.f;
+
+// The kernel's arguments, read again: what one tile size needs of them is not kept in
+// scalar registers for the others (up to 70 were spilled, into the inner loops too).
+__device__ __forceinline__ AttendArgs again() {
+    typedef const __attribute__((address_space(4))) AttendArgs* Constant;
+    Constant p = (Constant)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const AttendArgs*)p;
+}
 
 // The lane, of which the compiler knows nothing: what follows from it is worked out for
 // each item anew and not kept in registers beside the other tile sizes' values (they
@@ -593,7 +602,8 @@ __device__ __forceinline__ float reference(float top, float scale) {
 // without a stop in LDS.  HBM bounds it; a wave keeps the loads of its next 16 KB in
 // flight while it computes (bf16 at dim 128: 32 keys a step).
 template <class T, int kDim, bool kE4m3, bool kWide>
-__device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds) {
+__device__ void few_rows(const Item& s, unsigned head, char* lds) {
+    const AttendArgs A = again();
     typedef Keys<T, kDim, kE4m3> K;
     typedef typename K::P P;
     constexpr int kCols = K::kCols, kFrags = K::kFrags;
@@ -668,16 +678,20 @@ __device__ void few_rows(const AttendArgs& A, const Item& s, unsigned head, char
         }
         const u64 all = kSub == 4 ? ~0ull : (1ull << (16 * kSub)) - 1;
         if ((t.there & all) != all || (own && key0 + 16 * kSub > lim_all)) {
+            // key i of the lane is seen below its row's limit (a few at a time: the compiler
+            // would else hold all comparisons in scalar registers)
+            const int rest = own ? lim - (int)(key0 + 4 * quad) : 64;
 #pragma unroll
             for (int j = 0; j < kSub; ++j) {
                 const unsigned bits = (unsigned)(t.there >> (16 * j + 4 * quad)) & 15u;
                 clear_values(t.x[j], bits);
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (!(bits >> c & 1) || (own && (int)(key0 + 16 * j + 4 * quad + c) >= lim)) {
-                        st[j][c] = -INFINITY;
-                        if constexpr (kE4m3) t.x[j].vs[c] = 0.f;
-                    }
+                for (int c = 0; c < 4; ++c) {
+                    const bool seen = (bits >> c & 1) && 16 * j + c < rest;
+                    st[j][c] = seen ? st[j][c] : -INFINITY;
+                    if constexpr (kE4m3) t.x[j].vs[c] = seen ? t.x[j].vs[c] : 0.f;
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         float best = -INFINITY;
@@ -880,7 +894,8 @@ struct Straight {
     static constexpr unsigned kTurn = kPieces < 16 ? 3 : 7;       // pieces are turned in pairs
     unsigned lane, wave, col, quad;
     __device__ Straight(const AttendArgs&, unsigned l, unsigned w) : lane(l), wave(w), col(l % 16), quad(l / 16) {}
-    static __device__ void bring(const char* from, char* to) {
+    typedef const __attribute__((address_space(1))) char* global;
+    static __device__ void bring(global from, char* to) {
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                          (__attribute__((address_space(3))) void*)to, 16, 0, 0);
     }
@@ -898,10 +913,10 @@ struct Straight {
             const u64 u = u0 < 0 ? 0 : u0;
             const unsigned tb = (unsigned)A.token_bytes;
             const u64 slot = (u64)(first & mask) * A.token_bytes + head_off;
-            const char* const kb = A.k + u * A.k_unit + slot;
-            const char* const vb = A.v + u * A.v_unit + slot;
+            const global kb = (global)(A.k + (u * A.k_unit + slot)), vb = (global)(A.v + (u * A.v_unit + slot));
+            const unsigned k_at = col * tb + 16 * quad;
 #pragma unroll
-            for (int f = 0; f < kFrags; ++f) bring(kb + (col * tb + 64 * f + 16 * quad), lk + f * 1024);
+            for (int f = 0; f < kFrags; ++f) bring(kb + 64 * f + k_at, lk + f * 1024);
 #pragma unroll
             for (unsigned n = 0; n < 16 / kRowsAtOnce; ++n) {
                 const unsigned key = n * kRowsAtOnce + lane / kPieces;
@@ -912,13 +927,13 @@ struct Straight {
             const u64 ku = (u64)__shfl(safe, 16 * wave + col);
             const char* const kb = A.k + ku * A.k_unit + (u64)((first + col) & mask) * A.token_bytes + head_off;
 #pragma unroll
-            for (int f = 0; f < kFrags; ++f) bring(kb + (64 * f + 16 * quad), lk + f * 1024);
+            for (int f = 0; f < kFrags; ++f) bring((global)(kb + (64 * f + 16 * quad)), lk + f * 1024);
 #pragma unroll
             for (unsigned n = 0; n < 16 / kRowsAtOnce; ++n) {
                 const unsigned key = n * kRowsAtOnce + lane / kPieces;
                 const u64 vu = (u64)__shfl(safe, 16 * wave + key);
-                bring(A.v + vu * A.v_unit + (u64)((first + key) & mask) * A.token_bytes + head_off +
-                          16 * (lane % kPieces ^ turn(key)), lv + n * 1024);
+                bring((global)(A.v + vu * A.v_unit + (u64)((first + key) & mask) * A.token_bytes + head_off +
+                               16 * (lane % kPieces ^ turn(key))), lv + n * 1024);
             }
         }
     }
@@ -957,7 +972,8 @@ struct Straight {
 // 64 keys and values comes into LDS once for the four waves.  From about 150 rows on
 // the products bound it, below HBM does.
 template <class T, int kDim, bool kE4m3, int kQ, class Blocks>
-__device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, char* lds0, char* lds1) {
+__device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) {
+    const AttendArgs A = again();
     typedef typename Keys<T, kDim, kE4m3>::P P;
     constexpr int kCols = kDim / 16, kFrags = kDim / 32;
     const unsigned lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -1042,15 +1058,19 @@ __device__ void many_rows(const AttendArgs& A, const Item& s, unsigned head, cha
         const bool own = b >= range.nb0;
         const unsigned key0 = key_of(b);
         if (there != ~0ull || (own && key0 + kBlock > lim_all)) {
+            // key i of the lane's 16 is seen below its row's limit (a few at a time: the
+            // compiler would else hold 64 comparisons in scalar registers)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const unsigned bits = (unsigned)(there >> (16 * j + 4 * quad)) & 15u;
+            for (int t = 0; t < kQ; ++t) {
+                const int rest = own ? lim[t] - (int)(key0 + 4 * quad) : 64;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned bits = (unsigned)(there >> (16 * j + 4 * quad));
 #pragma unroll
-                    for (int t = 0; t < kQ; ++t)
-                        if (!(bits >> c & 1) || (own && (int)(key0 + 16 * j + 4 * quad + c) >= lim[t]))
-                            st[t][j][c] = -INFINITY;
+                    for (int c = 0; c < 4; ++c)
+                        st[t][j][c] = (bits >> c & 1) && 16 * j + c < rest ? st[t][j][c] : -INFINITY;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
         unsigned w[kQ][4][2];
@@ -1151,27 +1171,44 @@ __global__ __launch_bounds__(kWaves * 64, kDim > 128 ? 1 : 2) void k_attend(Atte
     __shared__ __align__(16) char lds1[kBlocks];
     __shared__ unsigned s_ticket[2];
     const unsigned n = A.counts[0] * A.n_heads;
-    // Items are taken as workgroups get free.  Which workgroup computes an item changes
-    // nothing in its result.  The next number is asked for early and looked at late; asked
-    // for two ahead, with the item read one ahead, workgroups hold items that others
-    // could take (64 agents over 8,192 tokens 84 us, as it is 70 us).
-    unsigned it = blockIdx.x;
+    // Items are taken as workgroups get free, item i by XCD i % 8 first (workgroups go
+    // round the XCDs), so that tiles next to each other, which read the same keys, share a
+    // cache.  Which workgroup computes an item changes nothing in its result.  The next
+    // number is asked for early and looked at late; asked for two ahead, workgroups hold
+    // items that others could take (64 agents over 8,192 tokens 84 us, as it is 70 us).
+    unsigned it = blockIdx.x, xcd = blockIdx.x % kXcds;
     for (unsigned turn = 0; it < n; turn ^= 1) {
         unsigned ticket = 0;
-        if (threadIdx.x == 0) ticket = atomicAdd(A.taken, 1u);
+        if (threadIdx.x == 0) ticket = atomicAdd(&A.taken[16 * xcd], 1u);
         const unsigned head = it % A.n_heads;
         const Item s = A.items[it / A.n_heads];
         if (s.tile_rows == 16) {
-            few_rows<T, kDim, kE4m3, kWide>(A, s, head, lds);
+            few_rows<T, kDim, kE4m3, kWide>(s, head, lds);
         } else {
             typedef typename std::conditional<kFull, Straight<T, kDim, kWide>,
                                               ThroughRegisters<T, kDim, kE4m3, kWide>>::type Blocks;
-            if (kDim > 128 || s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Blocks>(A, s, head, lds, lds1);
-            else if constexpr (kDim <= 128) many_rows<T, kDim, kE4m3, 2, Blocks>(A, s, head, lds, lds1);
+            if (kDim > 128 || s.tile_rows == 64) many_rows<T, kDim, kE4m3, 1, Blocks>(s, head, lds, lds1);
+            else if constexpr (kDim <= 128) many_rows<T, kDim, kE4m3, 2, Blocks>(s, head, lds, lds1);
         }
-        if (threadIdx.x == 0) s_ticket[turn] = ticket;
+        if (threadIdx.x == 0) {
+            // the first gridDim.x items are the workgroups' own
+            ticket = gridDim.x + ticket * kXcds + xcd;
+            if (ticket >= n) {                  // then those of the XCD that has most left
+                unsigned least = ~0u, x = 0;
+                for (unsigned k = 0; k < kXcds; ++k) {
+                    const unsigned c = __hip_atomic_load(&A.taken[16 * k], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    if (c < least) {
+                        least = c;
+                        x = k;
+                    }
+                }
+                if (gridDim.x + least * kXcds + x < n)
+                    ticket = gridDim.x + atomicAdd(&A.taken[16 * x], 1u) * kXcds + x;
+            }
+            s_ticket[turn] = ticket;
+        }
         __syncthreads();
-        it = gridDim.x + s_ticket[turn];
+        it = s_ticket[turn];
     }
 }
 
@@ -1296,7 +1333,7 @@ struct Layout {
 Layout layout_of(u64 n_rows, u64 n_requests, u64 n_groups, u64 n_heads, u64 per, unsigned dim) {
     Layout l;
     const u64 n = n_requests + n_groups, rows = part_rows(n_rows, n_heads * per);
-    l.items = 256;
+    l.items = 1024;
     l.joins = up(l.items + sizeof(Item) * most_items(n_rows, n, per));
     l.stacks = up(l.joins + sizeof(JoinRow) * n_rows);
     l.ml = up(l.stacks + sizeof(Stack) * n_groups);
@@ -1431,7 +1468,7 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     A.q_flip = scale < 0.f ? 0x80008000u : 0u;
     char* ws = static_cast<char*>(workspace);
     A.counts = reinterpret_cast<unsigned*>(ws);
-    A.taken = A.counts + 8;
+    A.taken = A.counts + 64;
     A.items = reinterpret_cast<Item*>(ws + l.items);
     A.joins = reinterpret_cast<JoinRow*>(ws + l.joins);
     A.most_items = most_items(rows, batch->n_requests + batch->n_groups, n_q_heads / cache->n_heads);
