@@ -464,8 +464,8 @@ struct Places {
 
 // Loads the 16 keys and values from key `key0` (a multiple of 16) on, whose units
 // lie in lanes `at` .. at + 15 of `unit`; tokens that are away are read from unit 0.
-// kWide: pages of 16 tokens and more, so the 16 keys are of one unit and their
-// address is the same for all lanes but for a 32-bit offset.
+// kWide: pages of 16 tokens and more, so the 16 keys are of one unit, the same for all
+// lanes, and their addresses differ by a 32-bit offset.
 template <class T, int kDim, bool kE4m3, bool kWide>
 __device__ __forceinline__ void load_keys(const AttendArgs& A, const Places<T, kDim, kE4m3>& p,
                                           unsigned head, int unit, unsigned at, unsigned key0,
@@ -487,8 +487,7 @@ __device__ __forceinline__ void load_keys(const AttendArgs& A, const Places<T, k
         }
     };
     if constexpr (kWide) {
-        const int u0 = __builtin_amdgcn_readlane(unit, at);
-        const u64 u = u0 < 0 ? 0 : u0;
+        const u64 u = unit < 0 ? 0 : unit;
         const unsigned slot = key0 & mask;
         const char* kb = A.k + u * A.k_unit + head_off + (u64)slot * A.token_bytes;
         const char* vb = A.v + u * A.v_unit + head_off + (u64)slot * A.token_bytes;
@@ -633,32 +632,62 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
 
     const unsigned blocks = range.b1 > range.b0 + wave ? (range.b1 - range.b0 - wave + kWaves - 1) / kWaves : 0;
     const unsigned steps = blocks * kSteps;
-    // step i: its segment's first entry, first key, number of keys
+    // step i: whether its keys are own tokens, and the first of them
     auto where = [&](unsigned i, bool* own, unsigned* key0) {
         const unsigned b = range.b0 + wave + i / kSteps * kWaves;
         *own = b >= range.nb0;
         *key0 = (*own ? b - range.nb0 : b) * kBlock + i % kSteps * (16 * kSub);
     };
+    // The step's table entries.  Of pages of 16 tokens and more they are the same for all
+    // lanes and come through the scalar cache, so that the count of vector reads on their
+    // way is that of keys alone, and a step's can be waited for with the next one's out.
+    struct Entries {
+        int of[kWide ? kSub : 1];
+    };
     auto look_up = [&](unsigned i) {
         bool own;
         unsigned key0;
         where(i, &own, &key0);
-        return entry_of(A, own ? s.first[1] : s.first[0], key0 + lane % (16 * kSub),
-                       own ? range.most : s.keys[0]);
+        const u64 first = own ? s.first[1] : s.first[0];
+        const unsigned limit = own ? range.most : s.keys[0];
+        Entries e;
+        if constexpr (kWide) {
+            const auto units = (const __attribute__((address_space(4))) int*)A.tab.units;
+#pragma unroll
+            for (int j = 0; j < kSub; ++j) {
+                const unsigned key = key0 + 16 * j;
+                e.of[j] = key < limit ? units[first + (key >> A.shift)] : -1;
+            }
+        } else {
+            e.of[0] = entry_of(A, first, key0 + lane % (16 * kSub), limit);
+        }
+        return e;
     };
     struct Step {
         K x[kSub];
         u64 there;
     };
-    auto load = [&](unsigned i, int entry, Step& t) {
-        const int unit = unit_of(A, entry);
+    auto load = [&](unsigned i, const Entries& e, Step& t) {
         bool own;
         unsigned key0;
         where(i, &own, &key0);
-        t.there = __ballot(unit >= 0);
+        if constexpr (kWide) {
+            const unsigned limit = own ? range.most : s.keys[0];
+            t.there = 0;
 #pragma unroll
-        for (int j = 0; j < kSub; ++j)
-            load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * j, key0 + 16 * j, t.x[j]);
+            for (int j = 0; j < kSub; ++j) {
+                const int unit = unit_of(A, e.of[j]);
+                const unsigned key = key0 + 16 * j, tokens = unit >= 0 && key < limit ? min(limit - key, 16u) : 0;
+                t.there |= (u64)((1u << tokens) - 1u) << (16 * j);
+                load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 0, key, t.x[j]);
+            }
+        } else {
+            const int unit = unit_of(A, e.of[0]);
+            t.there = __ballot(unit >= 0);
+#pragma unroll
+            for (int j = 0; j < kSub; ++j)
+                load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * j, key0 + 16 * j, t.x[j]);
+        }
     };
     auto compute = [&](unsigned i, Step& t) {
         bool own;
@@ -732,34 +761,38 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
             }
         }
     };
-    // units are looked up two steps ahead of their use, keys asked for one ahead
-    // (where 64 KB of registers hold two steps)
-    if constexpr (kDim <= 128 || kE4m3) {
-        Step a, b;
-        int next = -1, after = -1;
-        if (steps > 0) next = look_up(0);
-        if (steps > 1) after = look_up(1);
-        if (steps > 0) load(0, next, a);
-        for (unsigned i = 0; i < steps; i += 2) {
-            next = after;
-            if (i + 2 < steps) after = look_up(i + 2);
-            if (i + 1 < steps) load(i + 1, next, b);
-            compute(i, a);
-            if (i + 1 >= steps) break;
-            next = after;
-            if (i + 3 < steps) after = look_up(i + 3);
-            if (i + 2 < steps) load(i + 2, next, a);
-            compute(i + 1, b);
-        }
-    } else {
-        int next = -1;
-        if (steps > 0) next = look_up(0);
-        for (unsigned i = 0; i < steps; ++i) {
-            const int entry = next;
-            if (i + 1 < steps) next = look_up(i + 1);
-            Step a;
-            load(i, entry, a);
-            compute(i, a);
+    // entries are looked up two steps ahead of their use, keys asked for one ahead (where
+    // 64 KB of registers hold two steps), with no condition in between that would make
+    // the number of reads on their way unknown
+    if (steps > 0) {
+        if constexpr (kDim <= 128 || kE4m3) {
+            Step a, b;
+            load(0, look_up(0), a);
+            Entries next = look_up(steps > 1 ? 1 : 0);
+            unsigned i = 0;
+            for (; i + 2 < steps; i += 2) {
+                const Entries after = look_up(i + 2);
+                load(i + 1, next, b);
+                compute(i, a);
+                next = look_up(i + 3 < steps ? i + 3 : i + 2);
+                load(i + 2, after, a);
+                compute(i + 1, b);
+            }
+            if (i + 1 < steps) {
+                load(i + 1, next, b);
+                compute(i, a);
+                compute(i + 1, b);
+            } else {
+                compute(i, a);
+            }
+        } else {
+            Entries next = look_up(0);
+            for (unsigned i = 0; i < steps; ++i) {
+                Step a;
+                load(i, next, a);
+                if (i + 1 < steps) next = look_up(i + 1);
+                compute(i, a);
+            }
         }
     }
     float sum = soft.sum;
@@ -831,7 +864,8 @@ struct ThroughRegisters {
     __device__ ThroughRegisters(const AttendArgs& A, unsigned l, unsigned w) : p(A, l), lane(l), wave(w) {}
     // Asks for the wave's keys of the block at key0 into buffer `to`.
     __device__ void ask(const AttendArgs& A, unsigned head, int unit, unsigned key0, char*) {
-        load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * wave, key0 + 16 * wave, x);
+        load_keys<T, kDim, kE4m3, kWide>(A, p, head, kWide ? __builtin_amdgcn_readlane(unit, 16 * wave) : unit,
+                                         16 * wave, key0 + 16 * wave, x);
     }
     // Has them in the buffer, for all waves; `there`: the block's keys that are tokens.
     __device__ void arrive(const AttendArgs& A, u64 there, char* to) {
