@@ -18,7 +18,6 @@ namespace ss {
 
 namespace {
 
-constexpr unsigned kTile = 16;          // rows of a tile of k_adapter_in
 constexpr int kThreads = 256;
 constexpr unsigned kOutCols = 512;      // columns of out per round of a workgroup, 128 a wave
 
@@ -37,6 +36,7 @@ struct AdapterArgs {
     const unsigned* agents;
     unsigned n_rows, n_requests;
     float* low;                         // [pieces][n_rows][rank]: parts of A x
+    int* unit_of;                       // [n_requests]: each request's adapter, -1 = away
     unsigned pieces, piece;             // pieces of n_in, and elements of one
     unsigned cols;                      // columns of out per workgroup
 };
@@ -65,65 +65,83 @@ __device__ inline int adapter_of(const AdapterArgs& A, unsigned r) {
     return A.unit < n ? A.tab.unit(first + A.unit) : -1;
 }
 
-// A workgroup per tile and piece.  kTiles = rank / 16 (rounded up) products of 16 ranks x 16
-// rows; the four waves take 32 elements of the piece in turn.
-template <class T, int kTiles>
+// A workgroup per tile of up to 16 kSub rows and piece.  kTiles = rank / 16 (rounded up)
+// products of 16 ranks x 16 rows for each 16 rows; the four waves take 32 elements of the
+// piece in turn, as many of their reads in flight as registers hold.
+template <class T, int kTiles, int kSub>
 __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
-    __shared__ __align__(16) f32x4 s_acc[3][kTiles][64];
+    __shared__ __align__(16) f32x4 s_acc[3][kTiles * kSub][64];
     unsigned r, row0;
-    const unsigned rows = tile_of<kTile>(A, blockIdx.x / A.pieces, &r, &row0), piece = blockIdx.x % A.pieces;
+    const unsigned piece = blockIdx.x % A.pieces;
+    const unsigned rows = tile_of<16 * kSub>(A, blockIdx.x / A.pieces, &r, &row0);
     if (!rows) return;
     const int unit = adapter_of(A, r);
+    if (threadIdx.x == 0) A.unit_of[r] = unit;          // the same from every tile and piece
     if (unit < 0) return;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned col = lane % 16, quad = lane / 16;
     const unsigned k0 = piece * A.piece, k1 = min(A.n_in, k0 + A.piece);
-    const char* xr = A.x + (u64)(row0 + (col < rows ? col : 0)) * A.x_row;
+    const char* xr[kSub];
+#pragma unroll
+    for (int s = 0; s < kSub; ++s)
+        xr[s] = A.x + (u64)(row0 + (16 * s + col < rows ? 16 * s + col : 0)) * A.x_row;
     const char* am = A.a + (u64)unit * A.a_unit;
     const char* ar[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
         ar[t] = am + (u64)(t * 16 + col < A.rank ? t * 16 + col : 0) * A.n_in * 2;
-    f32x4 acc[kTiles];
+    f32x4 acc[kTiles][kSub];
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) acc[t] = f32x4{0, 0, 0, 0};
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) acc[t][s] = f32x4{0, 0, 0, 0};
     const u32x4 zero = {0, 0, 0, 0};
-    // steps of 32 elements, as many reads in flight as registers hold
-    constexpr int kSteps = kTiles == 1 ? 8 : kTiles == 2 ? 4 : 2;
+    constexpr int kSteps = kTiles == 1 ? 8 : kTiles == 2 ? 4 : kTiles == 4 ? 2 : 1;
 #pragma unroll 1
     for (unsigned k = k0 + wave * 32; k < k1; k += 128 * kSteps) {
-        u32x4 xf[kSteps], af[kSteps][kTiles];
+        u32x4 xf[kSteps][kSub], af[kSteps][kTiles];
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
             const unsigned at = k + 128 * u + quad * 8;
             const u64 off = (u64)(at < k1 ? at : k0) * 2;
-            xf[u] = *reinterpret_cast<const u32x4*>(xr + off);
+#pragma unroll
+            for (int s = 0; s < kSub; ++s) xf[u][s] = *reinterpret_cast<const u32x4*>(xr[s] + off);
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) af[u][t] = *reinterpret_cast<const u32x4*>(ar[t] + off);
         }
 #pragma unroll
         for (int u = 0; u < kSteps; ++u) {
             const bool in = k + 128 * u + quad * 8 < k1;
-            if (!in || col >= rows) xf[u] = zero;
+#pragma unroll
+            for (int s = 0; s < kSub; ++s)
+                if (!in || 16 * s + col >= rows) xf[u][s] = zero;
 #pragma unroll
             for (int t = 0; t < kTiles; ++t) {
                 if (!in || t * 16 + col >= A.rank) af[u][t] = zero;
-                acc[t] = T::mma(af[u][t], xf[u], acc[t]);
+#pragma unroll
+                for (int s = 0; s < kSub; ++s) acc[t][s] = T::mma(af[u][t], xf[u][s], acc[t][s]);
             }
         }
     }
     if (wave) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) s_acc[wave - 1][t][lane] = acc[t];
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int s = 0; s < kSub; ++s) s_acc[wave - 1][t * kSub + s][lane] = acc[t][s];
     }
     __syncthreads();
-    if (wave || col >= rows) return;
-    float* to = A.low + ((u64)piece * A.n_rows + row0 + col) * A.rank;
+    if (wave) return;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-        const f32x4 s = acc[t] + s_acc[0][t][lane] + s_acc[1][t][lane] + s_acc[2][t][lane];
-        const unsigned rr = t * 16 + quad * 4;
-        if (rr < A.rank) *reinterpret_cast<f32x4*>(to + rr) = s;
+    for (int s = 0; s < kSub; ++s) {
+        if (16 * s + col >= rows) continue;
+        float* to = A.low + ((u64)piece * A.n_rows + row0 + 16 * s + col) * A.rank;
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            const int i = t * kSub + s;
+            const f32x4 sum = acc[t][s] + s_acc[0][i][lane] + s_acc[1][i][lane] + s_acc[2][i][lane];
+            const unsigned rr = t * 16 + quad * 4;
+            if (rr < A.rank) *reinterpret_cast<f32x4*>(to + rr) = sum;
+        }
     }
 }
 
@@ -145,7 +163,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
     const unsigned rows = tile_of<kRows>(A, blockIdx.x / parts, &r, &row0);
     if (!rows) return;
-    const int unit = adapter_of(A, r);
+    const int unit = A.unit_of[r];
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned col = lane % 16, quad = lane / 16;
@@ -296,7 +314,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_adapter_out_few(AdapterArgs A) 
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
     const unsigned rows = tile_of<kFewRows>(A, blockIdx.x / parts, &r, &row0);
     if (!rows) return;
-    const int unit = adapter_of(A, r);
+    const int unit = A.unit_of[r];
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = lane % kSplit, col = lane / kSplit * 8;          // ranks 8 c .., columns col ..
@@ -378,11 +396,12 @@ __global__ __launch_bounds__(kThreads, 3) void k_adapter_out_few(AdapterArgs A) 
 
 template <class T, int kSplit>
 void out_few_launch(const AdapterArgs& A, hipStream_t st) {
-    // two rounds a wave: a workgroup reads its way to the adapter before it streams, and
-    // more rounds leave too few workgroups
+    // two rounds a wave where there are workgroups enough: each reads its way to the
+    // adapter before it streams (256 rows x 14,336 columns: one round 44 us, two 38 us,
+    // four 40 us; 16 rows x 4,096: one 11.6 us, two 12.2 us)
     AdapterArgs B = A;
-    B.cols = 2 * 4 * 512 / kSplit;
-    const unsigned tiles = A.n_rows / kFewRows + A.n_requests;
+    const unsigned tiles = A.n_rows / kFewRows + A.n_requests, round = 4 * 512 / kSplit;
+    B.cols = (u64)tiles * ((A.n_out + round - 1) / round) >= 1024 ? 2 * round : round;
     hipLaunchKernelGGL((k_adapter_out_few<T, kSplit>), dim3((A.n_out + B.cols - 1) / B.cols * tiles),
                        dim3(kThreads), 0, st, B);
 }
@@ -405,17 +424,28 @@ void out_launch(const AdapterArgs& A, hipStream_t st) {
     else hipLaunchKernelGGL((k_adapter_out<T, kSub, false>), grid, block, 0, st, B);
 }
 
+// Whether requests fill tiles of 32 rows: A and B are then read half as often.
+bool long_rows(u64 n_rows, u64 n_requests) { return n_rows >= 24 * n_requests; }
+
+template <class T, int kSub>
+void in_launch(const AdapterArgs& A, hipStream_t st) {
+    const dim3 grid(A.pieces * (A.n_rows / (16 * kSub) + A.n_requests)), block(kThreads);
+    switch ((A.rank + 15) / 16) {
+        case 1: hipLaunchKernelGGL((k_adapter_in<T, 1, kSub>), grid, block, 0, st, A); break;
+        case 2: hipLaunchKernelGGL((k_adapter_in<T, 2, kSub>), grid, block, 0, st, A); break;
+        case 3:
+        case 4: hipLaunchKernelGGL((k_adapter_in<T, 4, kSub>), grid, block, 0, st, A); break;
+        default: hipLaunchKernelGGL((k_adapter_in<T, 8, kSub>), grid, block, 0, st, A); break;
+    }
+}
+
 template <class T>
 void adapter_launch(const AdapterArgs& A, hipStream_t st) {
-    const unsigned tiles = A.n_rows / kTile + A.n_requests;
-    const dim3 in(A.pieces * tiles), block(kThreads);
-    switch ((A.rank + 15) / 16) {
-        case 1: hipLaunchKernelGGL((k_adapter_in<T, 1>), in, block, 0, st, A); break;
-        case 2: hipLaunchKernelGGL((k_adapter_in<T, 2>), in, block, 0, st, A); break;
-        case 3:
-        case 4: hipLaunchKernelGGL((k_adapter_in<T, 4>), in, block, 0, st, A); break;
-        default: hipLaunchKernelGGL((k_adapter_in<T, 8>), in, block, 0, st, A); break;
+    if (long_rows(A.n_rows, A.n_requests)) {
+        in_launch<T, 2>(A, st);
+        return out_launch<T, 2>(A, st);
     }
+    in_launch<T, 1>(A, st);
     // up to two rows a request as a rule: no product of 16 rows is worth its reads
     if (A.n_rows <= 2ull * A.n_requests) {
         switch (A.rank) {
@@ -426,19 +456,26 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
             case 128: return out_few_launch<T, 16>(A, st);
         }
     }
-    // tiles of 32 rows where requests fill them: B is read half as often
-    if (A.n_rows >= 24ull * A.n_requests) out_launch<T, 2>(A, st);
-    else out_launch<T, 1>(A, st);
+    out_launch<T, 1>(A, st);
 }
 
 // n_in is cut into pieces of at least 256 elements (two rounds of the four waves)
-// until about 1,024 workgroups run, four a compute unit.
+// until about four workgroups a compute unit run, two for long rows, whose pieces cost
+// more to add up.
 void pieces_of(u64 n_rows, u64 n_requests, u64 n_in, unsigned* pieces, unsigned* piece) {
-    const u64 tiles = n_rows / kTile + n_requests;
-    const u64 want = std::max<u64>(1, std::min<u64>((1024 + tiles - 1) / tiles, (n_in + 255) / 256));
+    const bool rows = long_rows(n_rows, n_requests);
+    const u64 tiles = n_rows / (rows ? 32 : 16) + n_requests, most = rows ? 512 : 1024;
+    const u64 want = std::max<u64>(1, std::min<u64>((most + tiles - 1) / tiles, (n_in + 255) / 256));
     const u64 len = ((n_in + want - 1) / want + 127) / 128 * 128;
     *piece = (unsigned)len;
     *pieces = (unsigned)((n_in + len - 1) / len);
+}
+
+// The parts of A x, then the requests' units.
+u64 low_bytes(u64 n_rows, u64 n_requests, u64 n_in, u64 rank) {
+    unsigned pieces, piece;
+    pieces_of(n_rows, n_requests, n_in, &pieces, &piece);
+    return pieces * n_rows * rank * 4;
 }
 
 ss_status adapter_args(const ss_adapters* a) {
@@ -477,9 +514,7 @@ uint64_t ss_adapter_add_workspace(const ss_adapters* adapters, uint32_t n_rows, 
     if (adapter_args(adapters) != SS_OK || n_rows == 0 || n_requests == 0 || n_rows >= (1u << 31) ||
         n_requests >= (1u << 20))
         return 0;
-    unsigned pieces, piece;
-    pieces_of(n_rows, n_requests, adapters->n_in, &pieces, &piece);
-    return (uint64_t)pieces * n_rows * adapters->rank * 4;
+    return low_bytes(n_rows, n_requests, adapters->n_in, adapters->rank) + 4ull * n_requests;
 }
 
 ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, const void* x,
@@ -553,6 +588,8 @@ ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, con
     A.n_rows = batch->n_rows;
     A.n_requests = batch->n_requests;
     A.low = static_cast<float*>(workspace);
+    A.unit_of = reinterpret_cast<int*>(static_cast<char*>(workspace) +
+                                       low_bytes(rows, batch->n_requests, n_in, adapters->rank));
     pieces_of(rows, batch->n_requests, n_in, &A.pieces, &A.piece);
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (adapters->type == SS_BF16) adapter_launch<Bf16>(A, st);

@@ -57,6 +57,7 @@ __device__ __forceinline__ void store_past(u32x4 x, void* to) {
     __builtin_nontemporal_store(x, static_cast<u32x4*>(to));
 }
 
+
 // A pool's block table: agent a's logical unit j is units[off[a] + j].
 struct Table {
     const int* units;
