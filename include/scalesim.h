@@ -437,7 +437,9 @@ ss_status ss_interaction_distances_static(const int32_t* pos_xy, const uint32_t*
  * waiting, allocate nothing and may be captured into a graph.  Every array
  * is device memory of the current device, owned by the caller, and stays as it
  * is until the work has run; the structs themselves are host memory, read
- * during the call.  Calls whose work can overlap need workspaces of their own.
+ * during the call.  What a call writes overlaps nothing else that it is given,
+ * unless said.  Calls whose work can overlap need workspaces of their own, and so
+ * do graphs that were captured with them and can run at the same time.
  *
  * The host checks what it can see (pointers, sizes, strides): SS_ERR_ARG, and
  * nothing is queued.  Values in device arrays are not checked: where they break
@@ -488,14 +490,14 @@ typedef struct {
     const uint32_t* agents;         /* [n_requests]; ids >= n_agents: the agent is away   */
     const uint32_t* lens;           /* [n_requests] tokens of the agent after this step,
                                        the request's rows being the last of them: row i of
-                                       n holds token lens[r] - n + i.  (Not used by
-                                       ss_adapter_add.)                                   */
+                                       n holds token lens[r] - n + i.  Below 2^31 - 64 for
+                                       ss_prefix_attention; not used by ss_adapter_add.   */
     uint32_t n_groups;              /* 0 = no prefixes; < 2^20                            */
     uint32_t pad;
     const uint32_t* group_off;      /* [n_groups + 1] nondecreasing, <= n_requests: group g
                                        is requests group_off[g] .. group_off[g+1]         */
     const uint32_t* prefix_agents;  /* [n_groups]                                         */
-    const uint32_t* prefix_lens;    /* [n_groups] tokens                                  */
+    const uint32_t* prefix_lens;    /* [n_groups] tokens, below 2^31 - 64                 */
 } ss_batch;
 
 /* Write the rows' keys and values into their agents' pages.  k and v are
@@ -533,12 +535,13 @@ ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, v
  *              must be below 2^30;
  *              n_rows * n_q_heads must be below 2^30;
  *   lse        [n_rows][n_q_heads] floats, or NULL;
- *   scale      finite (1 / sqrt(head_dim) as a rule);
+ *   scale      finite, also times log2(e) (1 / sqrt(head_dim) as a rule);
  *   workspace  ss_prefix_attention_workspace(...) bytes (a bound over all
  *              lengths, 0 for arguments that the call refuses), 16-byte
  *              aligned, no initialisation needed.
  * Scores, softmax statistics and sums are held in 32 bits; the weights are
- * rounded to 16 bits for the product with the values. */
+ * rounded to 16 bits for the product with the values (to bf16 with SS_E4M3, for
+ * SS_F16 rows together with what that rounding leaves). */
 uint64_t ss_prefix_attention_workspace(const ss_kv_cache* cache, const ss_batch* batch,
                                        uint32_t n_q_heads);
 ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, const void* q,

@@ -65,6 +65,13 @@ __device__ inline int adapter_of(const AdapterArgs& A, unsigned r) {
     return A.unit < n ? A.tab.unit(first + A.unit) : -1;
 }
 
+// The unit that k_adapter_in noted.  Offsets that break the rules can show the kernels
+// different requests, so what was noted may be anything.
+__device__ inline int unit_of(const AdapterArgs& A, unsigned r) {
+    const int u = A.unit_of[r];
+    return u >= 0 && (u64)u < A.tab.capacity ? u : -1;
+}
+
 // A workgroup per tile of up to 16 kSub rows and piece.  kTiles = rank / 16 (rounded up)
 // products of 16 ranks x 16 rows for each 16 rows; the four waves take 32 elements of the
 // piece in turn, as many of their reads in flight as registers hold.
@@ -163,7 +170,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
     const unsigned rows = tile_of<kRows>(A, blockIdx.x / parts, &r, &row0);
     if (!rows) return;
-    const int unit = A.unit_of[r];
+    const int unit = unit_of(A, r);
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned col = lane % 16, quad = lane / 16;
@@ -314,7 +321,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_adapter_out_few(AdapterArgs A) 
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
     const unsigned rows = tile_of<kFewRows>(A, blockIdx.x / parts, &r, &row0);
     if (!rows) return;
-    const int unit = A.unit_of[r];
+    const int unit = unit_of(A, r);
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = lane % kSplit, col = lane / kSplit * 8;          // ranks 8 c .., columns col ..

@@ -95,7 +95,7 @@ constexpr unsigned kPlanThreads = 512;
 
 __device__ unsigned tokens_with_page(const AttendArgs& A, unsigned agent, unsigned len, u64* first) {
     const u64 most = (u64)A.tab.row(agent, first) << A.shift;
-    return (unsigned)(len < most ? len : most);
+    return (unsigned)std::min<u64>(std::min<u64>(len, most), 0x7fffffc0u);
 }
 
 __device__ unsigned blocks_of(const Stack& s) {
@@ -416,7 +416,20 @@ struct Keys {
     static constexpr int kCols = kDim / 16, kFrags = kDim / 32;
     static constexpr int kLoads = kE4m3 ? kFrags / 2 : kFrags;
     static constexpr int kWords = kE4m3 ? kCols / 4 : kCols / 2;
-    typedef typename std::conditional<kE4m3, Bf16, T>::type P;  // weights times scales need range
+    // Weights times the values' scales need bf16's range; for fp16 rows, whose outputs
+    // keep three more bits, what their rounding leaves is multiplied too (in bf16 alone
+    // the outputs were off by 1.5e-3 where plain 32-bit sums are by 2.1e-4).
+    typedef typename std::conditional<kE4m3, Bf16, T>::type P;
+    static constexpr int kParts = kE4m3 && std::is_same<T, F16>::value ? 2 : 1;
+    // The parts of four weights.
+    static __device__ __forceinline__ void weights(f32x4 e, unsigned (*w)[2]) {
+        w[0][0] = P::pack(e[0], e[1]);
+        w[0][1] = P::pack(e[2], e[3]);
+        if constexpr (kParts == 2) {
+            w[1][0] = P::pack(e[0] - P::lo(w[0][0]), e[1] - P::hi(w[0][0]));
+            w[1][1] = P::pack(e[2] - P::lo(w[0][1]), e[3] - P::hi(w[0][1]));
+        }
+    }
     typedef unsigned wide __attribute__((ext_vector_type(kWords == 1 ? 2 : kWords)));
     u32x4 k[kLoads];
     unsigned v[4][kWords];
@@ -733,7 +746,7 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
             for (int c = 0; c < kCols; ++c) o[c] *= shrink;
         }
         const float off = soft.offset(scale);
-        unsigned w[kSub][2];
+        unsigned w[kSub][K::kParts][2];
 #pragma unroll
         for (int j = 0; j < kSub; ++j) {
             f32x4 e;
@@ -743,12 +756,10 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
                 soft.sum += e[c];
             }
             if constexpr (kE4m3) e *= t.x[j].vs;
-            w[j][0] = P::pack(e[0], e[1]);
-            w[j][1] = P::pack(e[2], e[3]);
+            K::weights(e, w[j]);
         }
 #pragma unroll
         for (int j = 0; j < kSub; j += 2) {
-            const u32x4 pf = {w[j][0], w[j][1], w[j + 1][0], w[j + 1][1]};
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
                 const unsigned sel = c % 2 ? 0x07060302u : 0x05040100u;
@@ -757,7 +768,9 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
                                   __builtin_amdgcn_perm(x.value(3, c / 2), x.value(2, c / 2), sel),
                                   __builtin_amdgcn_perm(y.value(1, c / 2), y.value(0, c / 2), sel),
                                   __builtin_amdgcn_perm(y.value(3, c / 2), y.value(2, c / 2), sel)};
-                o[c] = P::mma(vf, pf, o[c]);
+#pragma unroll
+                for (int k = 0; k < K::kParts; ++k)
+                    o[c] = P::mma(vf, u32x4{w[j][k][0], w[j][k][1], w[j + 1][k][0], w[j + 1][k][1]}, o[c]);
             }
         }
     };
@@ -1008,7 +1021,8 @@ struct Straight {
 template <class T, int kDim, bool kE4m3, int kQ, class Blocks>
 __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) {
     const AttendArgs A = again();
-    typedef typename Keys<T, kDim, kE4m3>::P P;
+    typedef Keys<T, kDim, kE4m3> K;
+    typedef typename K::P P;
     constexpr int kCols = kDim / 16, kFrags = kDim / 32;
     const unsigned lane = own_lane(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned col = lane % 16, quad = lane / 16;
@@ -1107,7 +1121,7 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
                 }
             }
         }
-        unsigned w[kQ][4][2];
+        unsigned w[kQ][4][K::kParts][2];
 #pragma unroll
         for (int t = 0; t < kQ; ++t) {
             float best = -INFINITY;
@@ -1129,8 +1143,7 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
                     soft[t].sum += e[c];
                 }
                 if constexpr (kE4m3) e *= keys.scales(here, 1, 16 * j + 4 * quad);
-                w[t][j][0] = P::pack(e[0], e[1]);
-                w[t][j][1] = P::pack(e[2], e[3]);
+                K::weights(e, w[t][j]);
             }
         }
 #pragma unroll
@@ -1145,9 +1158,12 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
 #pragma unroll
             for (int g = 0; g < kGroup; ++g)
 #pragma unroll
-                for (int t = 0; t < kQ; ++t)
-                    o[t][c + g] = P::mma(vf[i % 2][g], u32x4{w[t][2 * h][0], w[t][2 * h][1], w[t][2 * h + 1][0],
-                                                             w[t][2 * h + 1][1]}, o[t][c + g]);
+                for (int k = 0; k < K::kParts; ++k)
+#pragma unroll
+                    for (int t = 0; t < kQ; ++t)
+                        o[t][c + g] = P::mma(vf[i % 2][g], u32x4{w[t][2 * h][k][0], w[t][2 * h][k][1],
+                                                                 w[t][2 * h + 1][k][0], w[t][2 * h + 1][k][1]},
+                                             o[t][c + g]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -1436,7 +1452,8 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
                               void* workspace, uint64_t workspace_bytes, void* stream) {
     ss_status s = attend_args(cache, batch, type, n_q_heads);
     if (s != SS_OK) return s;
-    if (!std::isfinite(scale)) return set_err(SS_ERR_ARG, "scale must be finite");
+    if (!std::isfinite(scale * 1.4426950408889634f))
+        return set_err(SS_ERR_ARG, "scale must be finite, also times log2(e)");
     if (batch->n_rows == 0 || batch->n_requests == 0) return SS_OK;
     const unsigned dim = cache->head_dim;
     const u64 rows = batch->n_rows;

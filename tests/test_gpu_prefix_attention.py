@@ -9,7 +9,8 @@ rounding at |score| <= 8, more below through e), weights by a factor e^e and, wh
 rounded, u16 (fp16 weights below 2^-14 by 2^-25 of the largest weight); sums of n
 terms in 32 bits add n 2^-24.  That makes
     (u16 + 4 e + (n + 64) 2^-24) sum w |v| + n 2^-25 max|v| [fp16] + out |o|.
-log-sums are off by 2 e + (n + 64) 2^-24 + 2^-22 |lse|."""
+With an e4m3 cache weights are rounded to bf16, for fp16 outputs together with what
+that rounding leaves, which makes u16 2^-8 or 2^-16.  log-sums are off by 2 e + (n + 64) 2^-24 + 2^-22 |lse|."""
 import numpy as np
 import pytest
 
@@ -87,7 +88,8 @@ def check(cache, batch, q, per, kind, got, lse, scale):
     terms = (count[:, None] + 64) * 2.0 ** -24
     stored = M.BF16 if cache.kind == M.E4M3 else kind
     value = M.from_bits(got[:n], kind)
-    tol = (M.HALF_STEP[stored] + 4 * e + terms)[..., None] * mag + M.HALF_STEP[kind] * np.abs(o)
+    u16 = M.HALF_STEP[stored] ** (2 if cache.kind == M.E4M3 and kind == M.F16 else 1)
+    tol = (u16 + 4 * e + terms)[..., None] * mag + M.HALF_STEP[kind] * np.abs(o)
     if stored == M.F16:
         tol = tol + count[:, None, None] * 2.0 ** -25 * big
     if kind == M.F16:
@@ -247,6 +249,40 @@ def test_many_requests():
     rows = np.minimum(lens, rng.integers(0, 3, n))
     run(cache, Batch(rows, range(n), lens, ([0, 5, 1200, 2400], [0, 1, 2], [int(x) for x in lens[:3]])),
         1, M.BF16)
+
+
+def test_many_groups():
+    """More groups than the planning workgroup has threads, of two requests each."""
+    rng = np.random.default_rng(13)
+    n = 600
+    lens = rng.integers(1, 30, 2 * n)
+    plens = rng.integers(0, 50, n)
+    cache = Cache(rng, np.concatenate([lens, plens]), page=16, heads=1, dim=16, kind=M.F16)
+    groups = (list(range(0, 2 * n + 1, 2)), list(range(2 * n, 3 * n)), [int(x) for x in plens])
+    run(cache, Batch([1] * (2 * n), range(2 * n), lens, groups), 1, M.F16)
+
+
+@pytest.mark.parametrize("n", [507, 508, 509])
+def test_at_the_planning_workgroups_size(n):
+    """n requests and 4 groups, one of them of a single request: 511, 512 and 513 stacks."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(1, 90, n)
+    cache = Cache(rng, np.concatenate([lens, [40, 64, 100, 200]]), page=16, heads=1, dim=16, kind=M.BF16)
+    groups = ([0, 100, 101, 300, n], [n, n + 1, n + 2, n + 3], [40, 64, 100, 200])
+    run(cache, Batch([1] * n, range(n), lens, groups), 2, M.BF16)
+
+
+def test_strides_of_zero_in_what_is_read():
+    """One query row for all rows and heads."""
+    rng = np.random.default_rng(14)
+    cache = Cache(rng, [30, 70], page=16, heads=2, dim=64, kind=M.BF16)
+    batch = Batch([1, 2], [0, 1], [30, 70])
+    one = rng.standard_normal((1, 1, 64))
+    q = Rows(3, 4, 64, M.BF16, values=np.broadcast_to(one, (3, 4, 64)))
+    want, lse = attend(cache, batch, q, 2, M.BF16, scale=0.2)
+    q.strides = (0, 0)
+    got, lse2 = attend(cache, batch, q, 2, M.BF16, scale=0.2)
+    assert np.array_equal(got, want) and np.array_equal(lse, lse2)
 
 
 def test_same_result_every_time_and_without_lse():

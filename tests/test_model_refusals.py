@@ -123,7 +123,7 @@ def test_rows_that_overlap_are_refused_where_they_are_written():
 @pytest.mark.parametrize("change,msg", [
     (dict(q=0), "q must be"), (dict(out=8), "out must be"), (dict(n_q_heads=3), "n_q_heads"),
     (dict(n_q_heads=0), "n_q_heads"), (dict(n_q_heads=65538), "n_q_heads"),
-    (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"),
+    (dict(scale=float("nan")), "scale"), (dict(scale=3e38), "scale"), (dict(scale=float("inf")), "scale"),
     (dict(out=P), "out overlaps q"), (dict(out=P + 1024), "out overlaps q"),
     (dict(out_strides=(64, 64)), "overlap"), (dict(q_strides=(4, 64)), "multiples of 8"),
     (dict(workspace=0), "workspace"), (dict(workspace=P + 4), "workspace"),
