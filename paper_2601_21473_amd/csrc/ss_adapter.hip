@@ -555,23 +555,23 @@ ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, con
     if (workspace_bytes < need)
         return set_err(SS_ERR_ARG, "workspace_bytes %llu < %llu", (unsigned long long)workspace_bytes,
                        (unsigned long long)need);
-    int dev = -1;
-    if ((s = current_device(&dev)) != SS_OK ||
+    DeviceMemory mem;
+    if ((s = mem.current()) != SS_OK ||
         (s = table_memory(adapters->units, adapters->agent_off, adapters->n_agents, adapters->n_entries,
-                          dev)) != SS_OK ||
-        (s = batch_memory(batch, false, false, dev)) != SS_OK)
+                          mem)) != SS_OK ||
+        (s = batch_memory(batch, false, false, mem)) != SS_OK)
         return s;
     const u64 last = adapters->capacity_units - 1;
-    if (!device_range_ok(adapters->a, last * adapters->a_unit_bytes + 2ull * adapters->rank * n_in, dev))
-        return device_error("adapters a", dev);
-    if (!device_range_ok(adapters->b, last * adapters->b_unit_bytes + 2ull * adapters->rank * n_out, dev))
-        return device_error("adapters b", dev);
-    if (!device_range_ok(x, x_bytes, dev)) return device_error("x", dev);
-    if (!device_range_ok(base, base_bytes, dev)) return device_error("base", dev);
-    if (!device_range_ok(out, out_bytes, dev)) return device_error("out", dev);
-    if (scales && !device_range_ok(scales, (u64)batch->n_requests * 4, dev))
-        return device_error("scales", dev);
-    if (!device_range_ok(workspace, need, dev)) return device_error("workspace", dev);
+    if (!mem.has(adapters->a, last * adapters->a_unit_bytes + 2ull * adapters->rank * n_in))
+        return device_error("adapters a", mem.dev);
+    if (!mem.has(adapters->b, last * adapters->b_unit_bytes + 2ull * adapters->rank * n_out))
+        return device_error("adapters b", mem.dev);
+    if (!mem.has(x, x_bytes)) return device_error("x", mem.dev);
+    if (!mem.has(base, base_bytes)) return device_error("base", mem.dev);
+    if (!mem.has(out, out_bytes)) return device_error("out", mem.dev);
+    if (scales && !mem.has(scales, (u64)batch->n_requests * 4))
+        return device_error("scales", mem.dev);
+    if (!mem.has(workspace, need)) return device_error("workspace", mem.dev);
     AdapterArgs A{};
     A.tab = table_of(adapters->units, adapters->agent_off, adapters->n_agents, adapters->n_entries,
                      adapters->capacity_units);

@@ -1471,16 +1471,16 @@ ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, c
     const u64 out_bytes = rows_bytes(rows, n_q_heads, dim, out_row_stride, out_head_stride);
     const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
     if (q0 < o0 + out_bytes && o0 < q0 + q_bytes) return set_err(SS_ERR_ARG, "out overlaps q");
-    int dev = -1;
-    if ((s = current_device(&dev)) != SS_OK || (s = cache_memory(cache, dev)) != SS_OK ||
-        (s = batch_memory(batch, true, true, dev)) != SS_OK)
+    DeviceMemory mem;
+    if ((s = mem.current()) != SS_OK || (s = cache_memory(cache, mem)) != SS_OK ||
+        (s = batch_memory(batch, true, true, mem)) != SS_OK)
         return s;
-    if (!device_range_ok(q, q_bytes, dev)) return device_error("q", dev);
-    if (!device_range_ok(out, out_bytes, dev)) return device_error("out", dev);
-    if (lse && !device_range_ok(lse, rows * n_q_heads * 4, dev)) return device_error("lse", dev);
-    if (!device_range_ok(workspace, l.bytes, dev)) return device_error("workspace", dev);
+    if (!mem.has(q, q_bytes)) return device_error("q", mem.dev);
+    if (!mem.has(out, out_bytes)) return device_error("out", mem.dev);
+    if (lse && !mem.has(lse, rows * n_q_heads * 4)) return device_error("lse", mem.dev);
+    if (!mem.has(workspace, l.bytes)) return device_error("workspace", mem.dev);
     int cus = 256;
-    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) {
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, mem.dev) != hipSuccess) {
         (void)hipGetLastError();
         cus = 256;
     }

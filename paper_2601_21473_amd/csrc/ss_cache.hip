@@ -225,13 +225,13 @@ ss_status cache_call(const ss_kv_cache* c, const ss_batch* b, const void* k, con
                       !kWrite);
         if (s != SS_OK) return s;
     }
-    int dev = -1;
-    if ((s = current_device(&dev)) != SS_OK || (s = cache_memory(c, dev)) != SS_OK ||
-        (s = batch_memory(b, true, false, dev)) != SS_OK)
+    DeviceMemory mem;
+    if ((s = mem.current()) != SS_OK || (s = cache_memory(c, mem)) != SS_OK ||
+        (s = batch_memory(b, true, false, mem)) != SS_OK)
         return s;
     const u64 bytes = rows_bytes(b->n_rows, c->n_heads, c->head_dim, row_stride, head_stride);
-    if (!device_range_ok(k, bytes, dev)) return device_error("k", dev);
-    if (!device_range_ok(v, bytes, dev)) return device_error("v", dev);
+    if (!mem.has(k, bytes)) return device_error("k", mem.dev);
+    if (!mem.has(v, bytes)) return device_error("v", mem.dev);
     CacheArgs A{};
     A.tab = table_of(c->units, c->agent_off, c->n_agents, c->n_entries, c->capacity_units);
     A.plane[0] = static_cast<char*>(c->k);
@@ -385,46 +385,61 @@ u64 rows_bytes(u64 n_rows, u64 n_heads, u64 dim, u64 row_stride, u64 head_stride
     return n > (1ull << 61) ? UINT64_MAX : 2 * n;
 }
 
-ss_status current_device(int* dev) {
-    if (hipGetDevice(dev) != hipSuccess) {
+ss_status DeviceMemory::current() {
+    if (hipGetDevice(&dev) != hipSuccess) {
         (void)hipGetLastError();
         return set_err(SS_ERR_ARG, "no current device");
     }
     return SS_OK;
 }
 
+bool DeviceMemory::has(const void* ptr, u64 bytes) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(ptr);
+    for (int i = 0; i < n_known_; ++i)
+        if (p >= known_[i].base && p <= known_[i].end && bytes <= known_[i].end - p) return true;
+    if (!device_range_ok(ptr, bytes, dev)) return false;
+    hipDeviceptr_t base = nullptr;
+    size_t size = 0;
+    if (hipMemGetAddressRange(&base, &size, const_cast<void*>(ptr)) != hipSuccess) {
+        (void)hipGetLastError();                // managed memory, say
+    } else if (n_known_ < 4) {
+        known_[n_known_++] = {reinterpret_cast<uintptr_t>(base), reinterpret_cast<uintptr_t>(base) + size};
+    }
+    return true;
+}
+
 ss_status table_memory(const int32_t* units, const uint64_t* agent_off, uint32_t n_agents,
-                       uint64_t n_entries, int dev) {
-    if (!device_range_ok(units, n_entries * 4, dev)) return device_error("units", dev);
-    if (!device_range_ok(agent_off, ((u64)n_agents + 1) * 8, dev))
-        return device_error("agent_off", dev);
+                       uint64_t n_entries, DeviceMemory& mem) {
+    if (!mem.has(units, n_entries * 4)) return device_error("units", mem.dev);
+    if (!mem.has(agent_off, ((u64)n_agents + 1) * 8))
+        return device_error("agent_off", mem.dev);
     return SS_OK;
 }
 
-ss_status cache_memory(const ss_kv_cache* c, int dev) {
-    const ss_status s = table_memory(c->units, c->agent_off, c->n_agents, c->n_entries, dev);
+ss_status cache_memory(const ss_kv_cache* c, DeviceMemory& mem) {
+    const ss_status s = table_memory(c->units, c->agent_off, c->n_agents, c->n_entries, mem);
     if (s != SS_OK) return s;
     const u64 span = unit_span(c);
-    if (!device_range_ok(c->k, madd(span, c->capacity_units - 1, c->k_unit_bytes), dev))
-        return device_error("cache k", dev);
-    if (!device_range_ok(c->v, madd(span, c->capacity_units - 1, c->v_unit_bytes), dev))
-        return device_error("cache v", dev);
+    if (!mem.has(c->k, madd(span, c->capacity_units - 1, c->k_unit_bytes)))
+        return device_error("cache k", mem.dev);
+    if (!mem.has(c->v, madd(span, c->capacity_units - 1, c->v_unit_bytes)))
+        return device_error("cache v", mem.dev);
     return SS_OK;
 }
 
-ss_status batch_memory(const ss_batch* b, bool lens, bool groups, int dev) {
-    if (!device_range_ok(b->row_off, ((u64)b->n_requests + 1) * 4, dev))
-        return device_error("row_off", dev);
-    if (!device_range_ok(b->agents, (u64)b->n_requests * 4, dev)) return device_error("agents", dev);
-    if (lens && !device_range_ok(b->lens, (u64)b->n_requests * 4, dev))
-        return device_error("lens", dev);
+ss_status batch_memory(const ss_batch* b, bool lens, bool groups, DeviceMemory& mem) {
+    if (!mem.has(b->row_off, ((u64)b->n_requests + 1) * 4))
+        return device_error("row_off", mem.dev);
+    if (!mem.has(b->agents, (u64)b->n_requests * 4)) return device_error("agents", mem.dev);
+    if (lens && !mem.has(b->lens, (u64)b->n_requests * 4))
+        return device_error("lens", mem.dev);
     if (!groups || b->n_groups == 0) return SS_OK;
-    if (!device_range_ok(b->group_off, ((u64)b->n_groups + 1) * 4, dev))
-        return device_error("group_off", dev);
-    if (!device_range_ok(b->prefix_agents, (u64)b->n_groups * 4, dev))
-        return device_error("prefix_agents", dev);
-    if (!device_range_ok(b->prefix_lens, (u64)b->n_groups * 4, dev))
-        return device_error("prefix_lens", dev);
+    if (!mem.has(b->group_off, ((u64)b->n_groups + 1) * 4))
+        return device_error("group_off", mem.dev);
+    if (!mem.has(b->prefix_agents, (u64)b->n_groups * 4))
+        return device_error("prefix_agents", mem.dev);
+    if (!mem.has(b->prefix_lens, (u64)b->n_groups * 4))
+        return device_error("prefix_lens", mem.dev);
     return SS_OK;
 }
 

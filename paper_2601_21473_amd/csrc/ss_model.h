@@ -109,12 +109,22 @@ ss_status table_args(const int32_t* units, const uint64_t* agent_off, uint32_t n
                      uint64_t n_entries, uint64_t capacity_units);
 ss_status cache_args(const ss_kv_cache* cache, uint32_t row_type);
 ss_status batch_args(const ss_batch* batch, bool lens, bool groups);
-// Arrays in memory of the current device (*dev): the table and the planes, the batch.
+// The current device's memory, for one call's checks: arrays in an allocation that the
+// call has already asked the runtime about are not asked about again.
+class DeviceMemory {
+public:
+    ss_status current();                        // takes the current device
+    bool has(const void* ptr, u64 bytes);       // [ptr, ptr + bytes) in one allocation of it
+    int dev = -1;
+private:
+    struct { uintptr_t base, end; } known_[4];
+    int n_known_ = 0;
+};
+// Arrays in memory of the device: the table and the planes, the batch.
 ss_status table_memory(const int32_t* units, const uint64_t* agent_off, uint32_t n_agents,
-                       uint64_t n_entries, int dev);
-ss_status cache_memory(const ss_kv_cache* cache, int dev);
-ss_status batch_memory(const ss_batch* batch, bool lens, bool groups, int dev);
-ss_status current_device(int* dev);
+                       uint64_t n_entries, DeviceMemory& mem);
+ss_status cache_memory(const ss_kv_cache* cache, DeviceMemory& mem);
+ss_status batch_memory(const ss_batch* batch, bool lens, bool groups, DeviceMemory& mem);
 // Rows [n_rows][n_heads][dim] of 16-bit values: strides, alignment and extent.
 ss_status rows_args(const char* name, const void* ptr, u64 n_rows, u64 n_heads, u64 dim,
                     u64 row_stride, u64 head_stride, bool written);
