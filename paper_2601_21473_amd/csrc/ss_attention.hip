@@ -479,22 +479,28 @@ struct Places {
 // lie in lanes `at` .. at + 15 of `unit`; tokens that are away are read from unit 0.
 // kWide: pages of 16 tokens and more, so the 16 keys are of one unit, the same for all
 // lanes, and their addresses differ by a 32-bit offset.
-template <class T, int kDim, bool kE4m3, bool kWide>
+// kOnce: no other item reads them, so they go past the caches (131,071 tokens of one
+// agent 111 us, through them 116 us).
+template <class T, int kDim, bool kE4m3, bool kWide, bool kOnce>
 __device__ __forceinline__ void load_keys(const AttendArgs& A, const Places<T, kDim, kE4m3>& p,
                                           unsigned head, int unit, unsigned at, unsigned key0,
                                           Keys<T, kDim, kE4m3>& x) {
     typedef Keys<T, kDim, kE4m3> K;
     const unsigned mask = (1u << A.shift) - 1u;
     const u64 head_off = (u64)head * A.head_bytes;
+    auto read_once = [](auto* from) {
+        if constexpr (kOnce) return __builtin_nontemporal_load(from);
+        else return *from;
+    };
     auto k_from = [&](const char* row) {
 #pragma unroll
-        for (int f = 0; f < K::kLoads; ++f) x.k[f] = *reinterpret_cast<const u32x4*>(row + p.kd[f]);
+        for (int f = 0; f < K::kLoads; ++f) x.k[f] = read_once(reinterpret_cast<const u32x4*>(row + p.kd[f]));
     };
     auto v_from = [&](const char* row, int i) {
         if constexpr (K::kWords == 1) {
             x.v[i][0] = *reinterpret_cast<const unsigned*>(row);
         } else {
-            const typename K::wide w = *reinterpret_cast<const typename K::wide*>(row);
+            const typename K::wide w = read_once(reinterpret_cast<const typename K::wide*>(row));
 #pragma unroll
             for (int j = 0; j < K::kWords; ++j) x.v[i][j] = w[j];
         }
@@ -692,14 +698,14 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
                 const int unit = unit_of(A, e.of[j]);
                 const unsigned key = key0 + 16 * j, tokens = unit >= 0 && key < limit ? min(limit - key, 16u) : 0;
                 t.there |= (u64)((1u << tokens) - 1u) << (16 * j);
-                load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 0, key, t.x[j]);
+                load_keys<T, kDim, kE4m3, kWide, true>(A, p, head, unit, 0, key, t.x[j]);
             }
         } else {
             const int unit = unit_of(A, e.of[0]);
             t.there = __ballot(unit >= 0);
 #pragma unroll
             for (int j = 0; j < kSub; ++j)
-                load_keys<T, kDim, kE4m3, kWide>(A, p, head, unit, 16 * j, key0 + 16 * j, t.x[j]);
+                load_keys<T, kDim, kE4m3, kWide, true>(A, p, head, unit, 16 * j, key0 + 16 * j, t.x[j]);
         }
     };
     auto compute = [&](unsigned i, Step& t) {
@@ -877,7 +883,7 @@ struct ThroughRegisters {
     __device__ ThroughRegisters(const AttendArgs& A, unsigned l, unsigned w) : p(A, l), lane(l), wave(w) {}
     // Asks for the wave's keys of the block at key0 into buffer `to`.
     __device__ void ask(const AttendArgs& A, unsigned head, int unit, unsigned key0, char*) {
-        load_keys<T, kDim, kE4m3, kWide>(A, p, head, kWide ? __builtin_amdgcn_readlane(unit, 16 * wave) : unit,
+        load_keys<T, kDim, kE4m3, kWide, false>(A, p, head, kWide ? __builtin_amdgcn_readlane(unit, 16 * wave) : unit,
                                          16 * wave, key0 + 16 * wave, x);
     }
     // Has them in the buffer, for all waves; `there`: the block's keys that are tokens.
