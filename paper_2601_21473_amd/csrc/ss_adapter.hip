@@ -156,15 +156,16 @@ __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
 // 512 of them.  A x enters as two 16-bit parts, the rounded value and what the rounding left,
 // so that its 32 bits count for 16 (bf16) or 22 (fp16) of them; for fp16 each row is
 // first divided by a power of two near its largest value, as sums can pass that type's
-// range.  Up to rank 16 both parts fit next to each other into one product's 32 summed
-// indices, and the rows of B are read for both.
+// range.  Up to rank 16 the summed indices behind the last rank are zeros that cost no
+// reads (both parts side by side in one product, B read for each: 64 requests of 24 rows x
+// 14,336 columns 48 us, as it is 44 us).
 // Column n0 + 8 (lane % 16) + j is that of product j, so a lane ends up with eight
 // columns next to each other of four rows and moves them in 16 bytes, with nothing
 // exchanged.  HBM bounds it: base and B are asked for before the wait for A x.
-template <class T, int kSub, bool kPacked>
+template <class T, int kSub>
 __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(AdapterArgs A) {
-    constexpr unsigned kRows = 16 * kSub, kPitch = kPacked ? 40 : 2 * 128 + 8;
-    __shared__ __align__(16) unsigned short s_h[kRows][kPitch];     // two parts, zeros behind
+    constexpr unsigned kRows = 16 * kSub, kPitch = 2 * 128 + 8;
+    __shared__ __align__(16) unsigned short s_h[kRows][kPitch];     // ranks up to 128, their rests
     __shared__ float s_scale[kRows];
     unsigned r, row0;
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
@@ -189,11 +190,11 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
                     base[s][i] = *reinterpret_cast<const u32x4*>(A.base + (u64)(row0 + t) * A.base_row + (u64)n * 2);
             }
     };
-    // eight ranks of columns n .. n + 7 in step k: packed, ranks and parts go round
+    // eight ranks of columns n .. n + 7 in step k
     auto load_b = [&](unsigned n, unsigned k, u32x4* b) {
-        const unsigned c = 4 * k + quad, from = kPacked && c >= rank8 ? c - rank8 : c;
-        const bool there = n < n1 && from < rank8;
-        const unsigned at = there ? (n * rank8 + from) * 16 : 0;         // below 2^31
+        const unsigned c = 4 * k + quad;
+        const bool there = n < n1 && c < rank8;
+        const unsigned at = there ? (n * rank8 + c) * 16 : 0;            // below 2^31
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             b[j] = *reinterpret_cast<const u32x4*>(bm + (there ? at + j * A.rank * 2 : 0u));
@@ -246,16 +247,8 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
                                 fabsf(b) < INFINITY ? h[2 * j + 1] - b : 0.f);
             }
             const u32x4 high = {hi[0], hi[1], hi[2], hi[3]}, rest = {lo[0], lo[1], lo[2], lo[3]};
-            if constexpr (kPacked) {        // ranks, their rests, zeros up to 32
-                if (c < A.rank) {
-                    *reinterpret_cast<u32x4*>(&s_h[i][c]) = high;
-                    *reinterpret_cast<u32x4*>(&s_h[i][A.rank + c]) = rest;
-                }
-                if (2 * A.rank + c < 32) *reinterpret_cast<u32x4*>(&s_h[i][2 * A.rank + c]) = u32x4{0, 0, 0, 0};
-            } else {                        // ranks up to 128, then their rests (0 behind the last)
-                *reinterpret_cast<u32x4*>(&s_h[i][c]) = high;
-                *reinterpret_cast<u32x4*>(&s_h[i][128 + c]) = rest;
-            }
+            *reinterpret_cast<u32x4*>(&s_h[i][c]) = high;               // 0 behind the last rank
+            *reinterpret_cast<u32x4*>(&s_h[i][128 + c]) = rest;
         }
         __syncthreads();
     }
@@ -268,7 +261,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[t][j] = f32x4{0, 0, 0, 0};
         if (unit >= 0) {
-            const unsigned steps = kPacked ? 1 : (A.rank + 31) / 32;
+            const unsigned steps = (A.rank + 31) / 32;
 #pragma unroll 1
             for (unsigned k = 0; k < steps; ++k) {
 #pragma unroll
@@ -277,11 +270,9 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
                     const u32x4 high = *reinterpret_cast<const u32x4*>(h);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(high, bf[j], acc[t][j]);
-                    if constexpr (!kPacked) {
-                        const u32x4 rest = *reinterpret_cast<const u32x4*>(h + 128);
+                    const u32x4 rest = *reinterpret_cast<const u32x4*>(h + 128);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(rest, bf[j], acc[t][j]);
-                    }
+                    for (int j = 0; j < 8; ++j) acc[t][j] = T::mma(rest, bf[j], acc[t][j]);
                 }
                 if (k + 1 < steps) load_b(n, k + 1, bf);
                 else load_b(n + kOutCols, 0, bf);
@@ -427,12 +418,13 @@ void out_launch(const AdapterArgs& A, hipStream_t st) {
     AdapterArgs B = A;
     B.cols = kOutCols * each;
     const dim3 grid((pieces + each - 1) / each * tiles), block(kThreads);
-    if (A.rank <= 16) hipLaunchKernelGGL((k_adapter_out<T, kSub, true>), grid, block, 0, st, B);
-    else hipLaunchKernelGGL((k_adapter_out<T, kSub, false>), grid, block, 0, st, B);
+    hipLaunchKernelGGL((k_adapter_out<T, kSub>), grid, block, 0, st, B);
 }
 
-// Whether requests fill tiles of 32 rows: A and B are then read half as often.
-bool long_rows(u64 n_rows, u64 n_requests) { return n_rows >= 24 * n_requests; }
+// Whether requests have more rows than a tile of 16 as a rule: tiles of 32 then read A and
+// B half as often (4,096 x 14,336: 64 requests of 20 rows at rank 64 70 us, in tiles of 16
+// rows 93 us; of 24 rows at rank 16 44 and 58 us; of 16 rows 40 us, in tiles of 16 38 us).
+bool long_rows(u64 n_rows, u64 n_requests) { return n_rows > 16 * n_requests; }
 
 template <class T, int kSub>
 void in_launch(const AdapterArgs& A, hipStream_t st) {
