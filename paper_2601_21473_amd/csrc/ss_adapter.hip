@@ -3,7 +3,7 @@
 // for the rows t of each request r, with its agent's A [rank][n_in] and
 // B [n_out][rank] where the pool keeps them.
 //
-// Two kernels.  k_adapter_in computes A x in tiles of up to 16 rows of one request,
+// Two kernels.  k_adapter_in computes A x in tiles of up to 16 or 32 rows of one request,
 // the sum over n_in cut into pieces so that few rows still fill the card; the
 // pieces go to the workspace in 32 bits and k_adapter_out adds them up, in the same
 // order every time, when it loads them.  Both are matrix products of 16 x 16 x 32
@@ -302,8 +302,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
 // 32 bits: a column's ranks are in kSplit = rank / 8 lanes next to each other, each of
 // which takes eight columns in a row, so that the sums need log2(kSplit) exchanges and
 // leave in 16 bytes.  8 KB are in flight per wave while the 8 KB before are used
-// (as matrix products with two thirds of the lanes' reads doubled: 256 adapters of rank
-// 16 by 14,336 columns in 50 us).
+// (256 adapters of rank 16 by 14,336 columns: 26 us, as matrix products 38 us).
 constexpr unsigned kFewRows = 4;
 template <class T, int kSplit>
 __global__ __launch_bounds__(kThreads, 3) void k_adapter_out_few(AdapterArgs A) {
@@ -445,7 +444,10 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
         return out_launch<T, 2>(A, st);
     }
     in_launch<T, 1>(A, st);
-    // up to two rows a request as a rule: no product of 16 rows is worth its reads
+    // Up to two rows a request as a rule no product of 16 rows is worth its reads (256
+    // requests, 4,096 x 14,336, rank 16: one row 38 us, as products 49 us; two rows 50 and
+    // 54 us; three rows 63 and 59 us.  Rank 64, two rows: 145 and 152 us.  Only rank 32
+    // loses at two rows: 83 and 75 us).
     if (A.n_rows <= 2ull * A.n_requests) {
         switch (A.rank) {
             case 8: return out_few_launch<T, 1>(A, st);
@@ -459,8 +461,9 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
 }
 
 // n_in is cut into pieces of at least 256 elements (two rounds of the four waves)
-// until about four workgroups a compute unit run, two for long rows, whose pieces cost
-// more to add up.
+// until about four workgroups a compute unit run (256 adapters of 4,096 x 14,336: 38 us,
+// eight 47 us), two for long rows, whose pieces cost more to add up (8 prompts of 2,048 x
+// 8,192, rank 64: 54 us, one 57 us).
 void pieces_of(u64 n_rows, u64 n_requests, u64 n_in, unsigned* pieces, unsigned* piece) {
     const bool rows = long_rows(n_rows, n_requests);
     const u64 tiles = n_rows / (rows ? 32 : 16) + n_requests, most = rows ? 512 : 1024;

@@ -21,8 +21,12 @@ namespace {
 
 constexpr unsigned kNone = 0xffffffffu;
 constexpr unsigned kBlock = 64;             // keys of one step of an item
-constexpr unsigned kTarget = 1024;          // items that a call is split into at least, if it can
-constexpr unsigned kMinBlocks = 4;          // and key blocks that an item has at least
+// A call's items are about kTarget, twice the workgroups that run at a time, so that they
+// even out (64 agents over a prefix of 8,192: 1,024 items 70 us, 512 80 us, 2,048 78 us; one
+// of 131,071 tokens 121, 117 and 126 us), of kMinBlocks blocks at least (8: 72 us).
+constexpr unsigned kTarget = 1024;
+constexpr unsigned kAtOnce = 512;           // workgroups that run at a time: two a compute unit, dim 256 one
+constexpr unsigned kMinBlocks = 4;
 constexpr unsigned kXcds = 8;               // of the card, each with its own L2
 constexpr unsigned kMostRows = 128;         // rows of the largest tile
 
@@ -103,6 +107,8 @@ __device__ unsigned blocks_of(const Stack& s) {
 }
 // Rows of a stack's tiles: 16 while they hold all (nothing to share, so registers
 // suffice), else 64 or, where the registers hold the sums of so many, 128 through LDS.
+// (64 stacks over 4,000 keys of 8 heads of 128: 4 rows 187 us, in tiles of 64 202 us; 128
+// rows 204 us, in two tiles of 64 253 us; 256 rows 344 us, in four 445 us.)
 __device__ unsigned tile_rows(const AttendArgs& A, const Stack& s) {
     const u64 rows = (u64)s.rows * A.per;
     return rows <= 16 ? 16 : rows <= 64 || A.dim > 128 ? 64 : 128;
@@ -115,6 +121,9 @@ __device__ unsigned tiles_of(const AttendArgs& A, const Stack& s) {
 // The stack of group g's prefix.  It has rows (a stack of its own) where several
 // requests share the prefix and are so short that a tile of rows holds more than
 // one; otherwise each request reads prefix and own tokens in one go, without parts.
+// (64 requests of 8 heads of 128, 4 query heads each, over a prefix of 8,192: one row each
+// 51 us, without pools 226 us; 15 rows 194 and 235 us; 24 rows, so not pooled, 296 us, with
+// a pool 301 us, and over a prefix of 1,000 61 and 111 us.)
 __device__ Stack prefix_stack(const AttendArgs& A, unsigned g) {
     Stack t{};
     t.part = ~0ull;
@@ -276,11 +285,18 @@ __device__ void plan_stacks(const AttendArgs& A, Stack t, bool own, unsigned gro
 // joins carry all that their kernels need.
 __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
     __shared__ PlanState S;
-    __shared__ float s_work[kPlanThreads / 64];
+    __shared__ float s_work[kPlanThreads / 64][3];
     __shared__ unsigned s_rows[kPlanThreads / 64][2];
     const unsigned tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    // work in 32-bit floats: it only sets how fine the pieces are
-    float work = 0.f;
+    // in 32-bit floats, as they only set how fine the pieces are: key blocks of all tiles,
+    // tiles, and the most blocks that one has
+    float work = 0.f, tiles = 0.f, longest = 0.f;
+    auto count = [&](const Stack& t) {
+        const float n = (float)tiles_of(A, t), b = (float)blocks_of(t);
+        work += n * b;
+        tiles += n;
+        longest = fmaxf(longest, t.rows ? b : 0.f);
+    };
     unsigned own_rows = 0, pool_rows = 0;       // saturating: one of n_rows says enough
     auto add = [](unsigned a, unsigned b) { return a + b < a ? ~0u : a + b; };
     // Batches of up to kPlanThreads requests and groups: groups in the first threads,
@@ -305,45 +321,57 @@ __global__ __launch_bounds__(kPlanThreads) void k_attend_plan(AttendArgs A) {
         __syncthreads();
         if (is_request && n_groups)
             add_prefix(kPlanThreads - 1 - tid, n_groups, [&](unsigned g) { return S.at[0][g]; }, S.stack, mine);
-        work = (float)tiles_of(A, mine) * (float)blocks_of(mine);
+        count(mine);
     } else {
         for (unsigned g = tid; g < n_groups; g += kPlanThreads) {
             const Stack t = prefix_stack(A, g);
             A.stacks[g] = t;
-            work += (float)tiles_of(A, t) * (float)blocks_of(t);
+            count(t);
             pool_rows = add(pool_rows, t.rows);
         }
         __syncthreads();
         for (unsigned s = tid; s < n_requests; s += kPlanThreads) {
             Stack t = request_stack(A, s);
             add_prefix(s, n_groups, [&](unsigned g) { return A.group_off[g]; }, A.stacks, t);
-            work += (float)tiles_of(A, t) * (float)blocks_of(t);
+            count(t);
             own_rows = add(own_rows, t.rows);
         }
     }
 #pragma unroll
     for (int m = 32; m; m >>= 1) {
         work += __shfl_xor(work, m);
+        tiles += __shfl_xor(tiles, m);
+        longest = fmaxf(longest, __shfl_xor(longest, m));
         own_rows = add(own_rows, __shfl_xor(own_rows, m));
         pool_rows = add(pool_rows, __shfl_xor(pool_rows, m));
     }
     if (lane == 0) {
-        s_work[wave] = work;
+        s_work[wave][0] = work;
+        s_work[wave][1] = tiles;
+        s_work[wave][2] = longest;
         s_rows[wave][0] = own_rows;
         s_rows[wave][1] = pool_rows;
     }
     if (tid < 3) S.base[tid] = 0;
     __syncthreads();
-    work = 0.f;
+    work = tiles = 0.f;
     own_rows = pool_rows = 0;
 #pragma unroll
     for (unsigned w = 0; w < kPlanThreads / 64; ++w) {
-        work += s_work[w];
+        work += s_work[w][0];
+        tiles += s_work[w][1];
+        longest = fmaxf(longest, s_work[w][2]);
         own_rows = add(own_rows, s_rows[w][0]);
         pool_rows = add(pool_rows, s_rows[w][1]);
     }
     const float even = ceilf(work * (float)A.n_heads * (1.f / kTarget));
-    const unsigned chunk = even < (float)kMinBlocks ? kMinBlocks : even < 1e9f ? (unsigned)even : 1000000000u;
+    unsigned chunk = even < (float)kMinBlocks ? kMinBlocks : even < 1e9f ? (unsigned)even : 1000000000u;
+    // No piece at all where whole tiles, kAtOnce at a time, end within a tenth of the even
+    // share: parts cost what they write and the join reads (64 stacks of 128 rows over 4,000
+    // keys 204 us, in two pieces 282 us).
+    const float share = (float)A.n_heads * (A.dim > 128 ? 2.f / kAtOnce : 1.f / kAtOnce);
+    if (ceilf(tiles * share) * longest <= 1.1f * work * share)
+        chunk = std::max(chunk, (unsigned)longest);
     // offsets that give a row to two requests: nothing is computed
     if (own_rows <= A.n_rows && pool_rows <= A.n_rows) {
         // prefixes first: their items are the longest
@@ -1286,12 +1314,12 @@ __device__ __forceinline__ void join_row(const AttendArgs& A, unsigned w, float 
     float top = -INFINITY, sum = 0.f, x[kCols];
 #pragma unroll
     for (int c = 0; c < kCols; ++c) x[c] = 0.f;
-    constexpr int kAtOnce = kDim > 128 ? 4 : 8;
-    for (unsigned i0 = member; i0 < parts; i0 += kTeam * kAtOnce) {
-        float2 ml[kAtOnce];
-        float y[kAtOnce][kCols];
+    constexpr int kRead = kDim > 128 ? 4 : 8;
+    for (unsigned i0 = member; i0 < parts; i0 += kTeam * kRead) {
+        float2 ml[kRead];
+        float y[kRead][kCols];
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
+        for (int k = 0; k < kRead; ++k) {
             const unsigned i = min(i0 + k * kTeam, parts - 1);
             const u64 at = i < r.splits[0] ? first0 + (u64)i * r.total[0]
                                            : first1 + (u64)(i - r.splits[0]) * r.total[1];
@@ -1302,7 +1330,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& A, unsigned w, float 
         }
         float best = top;
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
+        for (int k = 0; k < kRead; ++k) {
             if (i0 + k * kTeam >= parts) ml[k] = float2{-INFINITY, 0.f};
             best = fmaxf(best, ml[k].x);
         }
@@ -1312,7 +1340,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& A, unsigned w, float 
 #pragma unroll
         for (int c = 0; c < kCols; ++c) x[c] *= shrink;
 #pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
+        for (int k = 0; k < kRead; ++k) {
             const float f = exp2f(ml[k].x - ref);
             sum += ml[k].y * f;
             // columns behind dim, and of a part that is not there, may hold anything

@@ -272,6 +272,21 @@ def test_at_the_planning_workgroups_size(n):
     run(cache, Batch([1] * n, range(n), lens, groups), 2, M.BF16)
 
 
+@pytest.mark.parametrize("n,heads,per,rows,dim", [
+    (64, 8, 2, 1, 64), (32, 8, 1, 1, 256), (64, 8, 4, 17, 64), (640, 1, 1, 1, 16)])
+def test_whole_tiles_that_fill_the_card(n, heads, per, rows, dim):
+    """Tiles enough that none is split, of the same length or nearly; one is much longer
+    or has no pages, and with it what is split changes."""
+    rng = np.random.default_rng(n + dim)
+    lens = 640 + rng.integers(0, 50, n)
+    for change in (None, 4000, 0):
+        if change is not None:
+            lens = lens.copy()
+            lens[n // 2] = change
+        cache = Cache(rng, lens, page=16, heads=heads, dim=dim, kind=M.BF16)
+        run(cache, Batch([rows] * n, range(n), lens), per, M.BF16)
+
+
 def test_strides_of_zero_in_what_is_read():
     """One query row for all rows and heads."""
     rng = np.random.default_rng(14)
