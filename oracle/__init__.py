@@ -6,6 +6,8 @@ moved) that the HIP library is compared against.  Only ``tests/``,
 ``__graft_entry__.smoke()`` and the CPU-baseline leg of ``bench.py`` may
 import it.  It shares no code with the HIP path; both read their inputs from
 the seeded generators in ``workloads``.
+``oracle.model`` has the 64-bit plain forms of the operators over resident
+units.
 
 Pins (see ``tests/test_oracle_*.py``): the paper's worked examples, Belady
 MIN and an exhaustive optimum on unit-size traces, an independent closed-form
