@@ -444,11 +444,12 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
         return out_launch<T, 2>(A, st);
     }
     in_launch<T, 1>(A, st);
-    // Up to two rows a request as a rule no product of 16 rows is worth its reads (256
-    // requests, 4,096 x 14,336, rank 16: one row 38 us, as products 49 us; two rows 50 and
-    // 54 us; three rows 63 and 59 us.  Rank 64, two rows: 145 and 152 us.  Only rank 32
-    // loses at two rows: 83 and 75 us).
-    if (A.n_rows <= 2ull * A.n_requests) {
+    // Up to one row a request as a rule no product of 16 rows is worth its reads (256
+    // requests, 4,096 x 14,336: rank 16 38 us, as products 49 us; 32 64 and 70 us; 64 114
+    // and 156 us; eight requests 12.0 and 11.5 us).  With two rows it wins less where there
+    // are many (256 requests: rank 16 50 and 54 us, 32 82 and 75 us, 64 145 and 152 us) than
+    // it loses where there are few (eight: 13.1 and 11.3 us, 17.6 and 12.0 us, 19.8 and 14.4 us).
+    if (A.n_rows <= A.n_requests) {
         switch (A.rank) {
             case 8: return out_few_launch<T, 1>(A, st);
             case 16: return out_few_launch<T, 2>(A, st);
