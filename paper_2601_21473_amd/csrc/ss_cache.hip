@@ -128,7 +128,7 @@ __global__ __launch_bounds__(kCacheThreads) void k_cache(CacheArgs A) {
     __shared__ u64 s_cell[2][16];               // byte offset of the row's token in its plane
     __shared__ u64 s_scale[2][16];
     __shared__ int s_state[16];                 // -2: no row, -1: away, 0: has a unit
-    const unsigned row0 = blockIdx.x * A.rows_per_block;
+    const unsigned row0 = workgroup() * A.rows_per_block;   // below 2^31 + 2^27
     {
         const unsigned i = threadIdx.x / 16, sub = threadIdx.x % 16;
         unsigned slot = 0;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kCacheThreads) void k_cache(CacheArgs A) {
 
 template <class T, bool kE4m3, bool kWrite>
 void cache_launch(const CacheArgs& A, hipStream_t st) {
-    const dim3 grid((A.n_rows + A.rows_per_block - 1) / A.rows_per_block), block(kCacheThreads);
+    const dim3 grid = grid_of((A.n_rows + A.rows_per_block - 1) / A.rows_per_block), block(kCacheThreads);
     if (A.dim <= 64) hipLaunchKernelGGL((k_cache<T, kE4m3, kWrite, 8>), grid, block, 0, st, A);
     else if (A.dim <= 128) hipLaunchKernelGGL((k_cache<T, kE4m3, kWrite, 16>), grid, block, 0, st, A);
     else hipLaunchKernelGGL((k_cache<T, kE4m3, kWrite, 32>), grid, block, 0, st, A);

@@ -57,6 +57,15 @@ __device__ __forceinline__ void store_past(u32x4 x, void* to) {
     __builtin_nontemporal_store(x, static_cast<u32x4*>(to));
 }
 
+// A launch's n workgroups (below 2^31), and which of them this one is.  A dimension of a grid
+// ends at 2^32 threads, and workgroups behind that are left out without an error, so more
+// than a row of them go into a second dimension; the last row's surplus workgroups have
+// numbers from n on.
+constexpr unsigned kGridRow = 1u << 23;
+inline dim3 grid_of(u64 n) {
+    return n <= kGridRow ? dim3((unsigned)n) : dim3(kGridRow, (unsigned)((n + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ unsigned workgroup() { return blockIdx.y * kGridRow + blockIdx.x; }
 
 // A pool's block table: agent a's logical unit j is units[off[a] + j].
 struct Table {
