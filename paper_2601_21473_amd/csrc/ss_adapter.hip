@@ -79,8 +79,8 @@ template <class T, int kTiles, int kSub>
 __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
     __shared__ __align__(16) f32x4 s_acc[3][kTiles * kSub][64];
     unsigned r, row0;
-    const unsigned piece = blockIdx.x % A.pieces;
-    const unsigned rows = tile_of<16 * kSub>(A, blockIdx.x / A.pieces, &r, &row0);
+    const unsigned piece = workgroup() % A.pieces;
+    const unsigned rows = tile_of<16 * kSub>(A, workgroup() / A.pieces, &r, &row0);
     if (!rows) return;
     const int unit = adapter_of(A, r);
     if (threadIdx.x == 0) A.unit_of[r] = unit;          // the same from every tile and piece
@@ -169,14 +169,14 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
     __shared__ float s_scale[kRows];
     unsigned r, row0;
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
-    const unsigned rows = tile_of<kRows>(A, blockIdx.x / parts, &r, &row0);
+    const unsigned rows = tile_of<kRows>(A, workgroup() / parts, &r, &row0);
     if (!rows) return;
     const int unit = unit_of(A, r);
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const unsigned col = lane % 16, quad = lane / 16;
-    const unsigned n0 = blockIdx.x % parts * A.cols + wave * 128;       // the wave's, the same
-    const unsigned n1 = min(A.n_out, blockIdx.x % parts * A.cols + A.cols);     // for all lanes
+    const unsigned n0 = workgroup() % parts * A.cols + wave * 128;       // the wave's, the same
+    const unsigned n1 = min(A.n_out, workgroup() % parts * A.cols + A.cols);     // for all lanes
     const unsigned rank8 = A.rank / 8;
     const char* const bm = A.b + (u64)(unit < 0 ? 0 : unit) * A.b_unit;
     auto load_base = [&](unsigned n, u32x4 (*base)[4]) {
@@ -309,14 +309,14 @@ __global__ __launch_bounds__(kThreads, 3) void k_adapter_out_few(AdapterArgs A) 
     constexpr unsigned kCols = 512 / kSplit;            // columns of a wave's round
     unsigned r, row0;
     const unsigned parts = (A.n_out + A.cols - 1) / A.cols;
-    const unsigned rows = tile_of<kFewRows>(A, blockIdx.x / parts, &r, &row0);
+    const unsigned rows = tile_of<kFewRows>(A, workgroup() / parts, &r, &row0);
     if (!rows) return;
     const int unit = unit_of(A, r);
     if (unit < 0 && A.base == A.out) return;
     const unsigned lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const unsigned c = lane % kSplit, col = lane / kSplit * 8;          // ranks 8 c .., columns col ..
-    const unsigned n0 = blockIdx.x % parts * A.cols + wave * kCols;
-    const unsigned n1 = min(A.n_out, blockIdx.x % parts * A.cols + A.cols);
+    const unsigned n0 = workgroup() % parts * A.cols + wave * kCols;
+    const unsigned n1 = min(A.n_out, workgroup() % parts * A.cols + A.cols);
     if (unit < 0) {
         for (unsigned n = n0 + lane * 8; n < n1; n += 4 * kCols)
             if (lane * 8 < kCols)
@@ -399,7 +399,7 @@ void out_few_launch(const AdapterArgs& A, hipStream_t st) {
     AdapterArgs B = A;
     const unsigned tiles = A.n_rows / kFewRows + A.n_requests, round = 4 * 512 / kSplit;
     B.cols = (u64)tiles * ((A.n_out + round - 1) / round) >= 1024 ? 2 * round : round;
-    hipLaunchKernelGGL((k_adapter_out_few<T, kSplit>), dim3((A.n_out + B.cols - 1) / B.cols * tiles),
+    hipLaunchKernelGGL((k_adapter_out_few<T, kSplit>), grid_of((A.n_out + B.cols - 1) / B.cols * tiles),
                        dim3(kThreads), 0, st, B);
 }
 
@@ -416,7 +416,7 @@ void out_launch(const AdapterArgs& A, hipStream_t st) {
     const unsigned each = std::max(1u, (pieces + want - 1) / want);
     AdapterArgs B = A;
     B.cols = kOutCols * each;
-    const dim3 grid((pieces + each - 1) / each * tiles), block(kThreads);
+    const dim3 grid = grid_of((pieces + each - 1) / each * tiles), block(kThreads);
     hipLaunchKernelGGL((k_adapter_out<T, kSub>), grid, block, 0, st, B);
 }
 
@@ -427,7 +427,7 @@ bool long_rows(u64 n_rows, u64 n_requests) { return n_rows > 16 * n_requests; }
 
 template <class T, int kSub>
 void in_launch(const AdapterArgs& A, hipStream_t st) {
-    const dim3 grid(A.pieces * (A.n_rows / (16 * kSub) + A.n_requests)), block(kThreads);
+    const dim3 grid = grid_of(A.pieces * (A.n_rows / (16 * kSub) + A.n_requests)), block(kThreads);
     switch ((A.rank + 15) / 16) {
         case 1: hipLaunchKernelGGL((k_adapter_in<T, 1, kSub>), grid, block, 0, st, A); break;
         case 2: hipLaunchKernelGGL((k_adapter_in<T, 2, kSub>), grid, block, 0, st, A); break;
