@@ -155,10 +155,11 @@ __global__ __launch_bounds__(kThreads) void k_adapter_in(AdapterArgs A) {
 // A workgroup per tile of up to 16 kSub rows and A.cols columns; a wave takes 128 of each
 // 512 of them.  A x enters as two 16-bit parts, the rounded value and what the rounding left,
 // so that its 32 bits count for 16 (bf16) or 22 (fp16) of them; for fp16 each row is
-// first divided by a power of two near its largest value, as sums can pass that type's
-// range.  Up to rank 16 the summed indices behind the last rank are zeros that cost no
-// reads (both parts side by side in one product, B read for each: 64 requests of 24 rows x
-// 14,336 columns 48 us, as it is 44 us).
+// first multiplied by a power of two that brings its largest value to 2^14 .. 2^15, as sums
+// can pass that type's range at both ends: values down to 2^-17 of the row's largest keep 22
+// bits, smaller ones are off by 2^-39 of it at most.  Up to rank 16 the summed indices
+// behind the last rank are zeros that cost no reads (both parts side by side in one product,
+// B read for each: 64 requests of 24 rows x 14,336 columns 48 us, as it is 44 us).
 // Column n0 + 8 (lane % 16) + j is that of product j, so a lane ends up with eight
 // columns next to each other of four rows and moves them in 16 bytes, with nothing
 // exchanged.  HBM bounds it: base and B are asked for before the wait for A x.
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
             float unscale = 1.f;
             if constexpr (std::is_same<T, F16>::value) {
                 if (top > 0.f && top < INFINITY) {
-                    const int e = min(max(ilogbf(top), -100), 100);
+                    const int e = min(max(ilogbf(top), -100), 100) - 14;
                     unscale = ldexpf(1.f, e);
                     const float s = ldexpf(1.f, -e);
 #pragma unroll

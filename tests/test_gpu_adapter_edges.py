@@ -16,6 +16,53 @@ def _gpu():
     assert B.device_count() > 0, "GPU tests need a GPU"
 
 
+def fill(ad, a, b):
+    """Every unit's matrices become a [rank, n_in] and b [n_out, rank]."""
+    for i, (held, x) in enumerate(((ad.a, a), (ad.b, b))):
+        held[:] = M.to_bits(x, ad.kind)
+        raw = np.zeros((len(held), ad.chunk[i]), np.uint8)
+        raw[:, :2 * x.size] = held.reshape(len(held), -1).view(np.uint8)
+        ad.bufs[i].upload(raw)
+
+
+@pytest.mark.parametrize("rows", [[1, 0, 1, 1], [2, 3], [20, 40, 1]])
+@pytest.mark.parametrize("rank", [16, 40])
+def test_fp16_sums_far_below_the_rows_largest(rows, rank):
+    """A x has an element of 1,024 times the row, which B does not use, beside elements
+    2^20 and more below it, which make the output.
+
+    A row of A x is held in two fp16 parts under a power of two that brings its largest to
+    2^14 at least.  A part's step below the normal range is 2^-24, so an element is off by
+    2^-22 of itself (two roundings to half a step, 2^-11) or by 2^-25 of 2^-14 of the largest, 2^-39;
+    B and the other terms as in test_gpu_adapters."""
+    rng = np.random.default_rng(rank)
+    n_in, n_out = 64, 264
+    ad = Adapters(rng, 4, rank, n_in, n_out, M.F16)
+    a, b = np.zeros((rank, n_in)), rng.uniform(1, 2, (n_out, rank))
+    a[0, 0], b[:, 0] = 1024.0, 0.0
+    a[1:, 1] = rng.uniform(1, 2, rank - 1) * 2.0 ** -10 * 2.0 ** -rng.integers(0, 4, rank - 1)
+    fill(ad, a, b)
+    batch = Batch(rows, range(len(rows)), [0] * len(rows))
+    x = np.zeros((batch.n_rows, 1, n_in))
+    x[:, 0, 0] = rng.choice([-1.0, 1.0, 2.0], batch.n_rows)
+    x[:, 0, 1] = rng.uniform(0.5, 1, batch.n_rows)
+    d_x = Rows(batch.n_rows, 1, n_in, M.F16, values=x)
+    base = Rows(batch.n_rows, 1, n_out, M.F16, values=np.zeros((batch.n_rows, 1, n_out)))
+    need = B.adapter_add_workspace(ad.desc, batch.n_rows, len(rows))
+    ws = DeviceBuffer(need)
+    B.adapter_add(ad.desc, batch.desc, d_x.ptr, base.ptr, base.ptr, x_stride=n_in, base_stride=n_out,
+                  out_stride=n_out, workspace=ws.ptr, workspace_bytes=need)
+    B.null_stream_sync()
+    xv = d_x.before()[:, 0]
+    am, bm = M.from_bits(ad.a[0], M.F16), M.from_bits(ad.b[0], M.F16)
+    want, second, first = M.adapter(xv, am, bm, 0.0, 1.0)
+    top = np.abs(xv @ am.T).max(-1)[:, None]
+    tol = 2.0 ** -11 * np.abs(want) + (2.0 ** -22 + (2 * rank + 8) * 2.0 ** -24) * second + \
+        (n_in + 40) * 2.0 ** -24 * first + 2.0 ** -39 * top * np.abs(bm).sum(1)[None] + 2.0 ** -25
+    err = np.abs(base.values()[:, 0] - want)
+    assert (err <= tol).all(), (err.max(), tol.min(), np.abs(want).min())
+
+
 def test_more_workgroups_than_one_grid_dimension():
     """2^20 - 1 requests, nearly all of no rows, over a wide projection: 58 million
     workgroups of 256 threads, where a dimension of a grid ends at 2^32 threads.  Bounds
