@@ -541,7 +541,8 @@ ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, v
  *              aligned, no initialisation needed.
  * Scores, softmax statistics and sums are held in 32 bits; the weights are
  * rounded to 16 bits for the product with the values (to bf16 with SS_E4M3, for
- * SS_F16 rows together with what that rounding leaves). */
+ * SS_F16 rows together with what that rounding leaves; fp16 weights below 2^-20
+ * of their row's largest are off by 2^-31 of it at most). */
 uint64_t ss_prefix_attention_workspace(const ss_kv_cache* cache, const ss_batch* batch,
                                        uint32_t n_q_heads);
 ss_status ss_prefix_attention(const ss_kv_cache* cache, const ss_batch* batch, const void* q,

@@ -449,6 +449,11 @@ struct Keys {
     // the outputs were off by 1.5e-3 where plain 32-bit sums are by 2.1e-4).
     typedef typename std::conditional<kE4m3, Bf16, T>::type P;
     static constexpr int kParts = kE4m3 && std::is_same<T, F16>::value ? 2 : 1;
+    // fp16 weights are held against 2^-kLift of the reference, 2^(kLift + kSlack) at most:
+    // held against the reference itself those below 2^-14 of it lost bits, and those below
+    // 2^-25 became nothing, which many of them together show (8,000 weights of 2^-25: the
+    // output was off by 3%).  Two powers of two stay free for the rounding of the exponents.
+    static constexpr float kLift = std::is_same<P, F16>::value ? 6.f : 0.f;
     // The parts of four weights.
     static __device__ __forceinline__ void weights(f32x4 e, unsigned (*w)[2]) {
         w[0][0] = P::pack(e[0], e[1]);
@@ -616,7 +621,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& A, const Item& s,
 }
 
 // Running reference and sum of one row's scores, and its weights.  `top` is an
-// unscaled score; weights are 2^(scale (score - top)).
+// unscaled score; weights are 2^(scale (score - top) + lift).
 struct Softmax {
     float top = -INFINITY, sum = 0.f;
     // Whether a score passes the reference by more than the slack (in some lane).
@@ -634,13 +639,16 @@ struct Softmax {
         sum *= shrink;
         return shrink;
     }
-    __device__ float offset(float scale) const { return top == -INFINITY ? 0.f : -top * scale; }
+    // What weights are relative to, in log2, -infinity without any score; `lift` lower than
+    // the reference itself.
+    __device__ float reference(float scale, float lift) const {
+        return top == -INFINITY ? -INFINITY : fmaf(top, scale, -lift);
+    }
+    // and what it adds to a score's exponent
+    __device__ float offset(float scale, float lift) const {
+        return top == -INFINITY ? 0.f : fmaf(-top, scale, lift);
+    }
 };
-
-// log2 of the reference's scale for a part: weights are relative to 2^this.
-__device__ __forceinline__ float reference(float top, float scale) {
-    return top == -INFINITY ? -INFINITY : top * scale;
-}
 
 // 16 rows and a range of keys.  The four waves take 64-key blocks in turn, each
 // with a reference and sum of its own, and join at the end: with so few rows a key
@@ -779,7 +787,7 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
 #pragma unroll
             for (int c = 0; c < kCols; ++c) o[c] *= shrink;
         }
-        const float off = soft.offset(scale);
+        const float off = soft.offset(scale, K::kLift);
         unsigned w[kSub][K::kParts][2];
 #pragma unroll
         for (int j = 0; j < kSub; ++j) {
@@ -845,7 +853,7 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
     float sum = soft.sum;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    const float top = reference(soft.top, scale);
+    const float top = soft.reference(scale, K::kLift);
 
     // join the four waves: lds_o[wave][row][kDim + 4], lds_ml[wave][row]
     constexpr int kPitch = kDim + 4;
@@ -1167,7 +1175,7 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) o[t][c] *= shrink;
             }
-            const float off = soft[t].offset(scale);
+            const float off = soft[t].offset(scale, K::kLift);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 f32x4 e;
@@ -1213,7 +1221,7 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
         float sum = soft[t].sum;
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        const float top = reference(soft[t].top, scale);
+        const float top = soft[t].reference(scale, K::kLift);
         if (m >= total) continue;
         const unsigned row = m / A.per, hh = head * A.per + (m - row * A.per);
         const float mine = direct ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
