@@ -508,7 +508,9 @@ typedef struct {
  *     s = max(largest finite |x| / 448, 2^-126)
  * and the codes x / s, rounded to nearest even; infinities become the largest
  * code, NaN stays NaN.  Rows whose unit is away or whose token is negative are
- * not written.  Two rows for one token: either may be the one that is kept. */
+ * not written.  Two rows of a call for one token (an agent in two requests) leave
+ * that token's key, value and scales in every head unspecified, all else as if
+ * they were one row. */
 ss_status ss_kv_write(const ss_kv_cache* cache, const ss_batch* batch, const void* k,
                       const void* v, uint32_t type, uint64_t row_stride, uint64_t head_stride,
                       void* stream);

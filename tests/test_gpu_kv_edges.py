@@ -62,3 +62,38 @@ def test_more_workgroups_than_one_grid_dimension(kind):
             assert (got == (want if there else 0)).all(), (first, there)
     for b in out + planes:
         b.free()
+
+
+@pytest.mark.parametrize("kind", [M.BF16, M.E4M3])
+def test_two_rows_for_one_token(kind):
+    """Agent 0 in three requests, two of which give it the same tokens: what those hold may be
+    anything, the other tokens and every byte beside them are as the rows say."""
+    rng = np.random.default_rng(2)
+    cache = Cache(rng, [40, 20], page=16, heads=3, dim=64, kind=kind)
+    batch = Batch([6, 9, 4, 2], [0, 1, 0, 0], [30, 20, 27, 40])
+    new = [Rows(batch.n_rows, 3, 64, M.BF16, values=rng.standard_normal((batch.n_rows, 3, 64)))
+           for _ in range(2)]
+    before = [b.copy() for b in cache.bytes]
+    B.kv_write(cache.desc, batch.desc, new[0].ptr, new[1].ptr, type=M.BF16, strides=new[0].strides)
+    B.null_stream_sync()
+    request, token = M.positions(batch.row_off, batch.lens)
+    twice = sorted(set(range(24, 30)) & set(range(23, 27)))
+    got = cache.download()
+    for i in range(2):
+        x = new[i].before()
+        want = before[i].copy()
+        for t in range(len(request)):
+            u, slot = cache.place(int(batch.agents[request[t]]), int(token[t]))
+            if kind == M.E4M3:
+                s = M.e4m3_scale(x[t])
+                cache.scale_view(want)[u, :, slot] = s
+                cache.body(want)[u, :, slot] = M.e4m3_encode(x[t].astype(np.float32) / s[:, None])
+            else:
+                cache.body(want)[u, :, slot] = new[i].view(new[i].bytes)[t]
+        for p in (got[i], want):
+            for token_twice in twice:
+                u, slot = cache.place(0, token_twice)
+                cache.body(p)[u, :, slot] = 0
+                if kind == M.E4M3:
+                    cache.scale_view(p)[u, :, slot] = 0
+        assert np.array_equal(got[i], want)
