@@ -377,6 +377,9 @@ class Pool:
             if offset < 0 or offset + need > int(self._chunk[plane]):
                 raise ValueError(f"a page of {need} bytes at {offset} does not fit into the "
                                  f"{int(self._chunk[plane])}-byte chunks of plane {plane}")
+        if k_plane == v_plane and abs(k_offset - v_offset) < need:
+            raise ValueError(f"keys at {k_offset} and values at {v_offset} of plane {k_plane} "
+                             f"overlap: a page takes {need} bytes")
         return kv_cache(**self._table(), k=self._bases[k_plane] + k_offset,
                         v=self._bases[v_plane] + v_offset, k_unit_bytes=self._chunk[k_plane],
                         v_unit_bytes=self._chunk[v_plane], page_tokens=page_tokens,
