@@ -18,7 +18,7 @@ def pool():
     return pool
 
 
-@pytest.mark.parametrize("k_offset,v_offset", [(0, 0), (0, 2048), (4096, 64), (64, 4144)])
+@pytest.mark.parametrize("k_offset,v_offset", [(0, 0), (0, 2048), (4096, 64), (64, 4080)])
 def test_keys_and_values_in_the_same_bytes(pool, k_offset, v_offset):
     """A page of 16 x 2 x 64 16-bit values is 4,096 bytes; keys and values may share a
     plane, not bytes of it."""
