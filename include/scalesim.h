@@ -524,7 +524,8 @@ ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, v
 /* Attention of a batch over its agents' pages.  Query head h of n_q_heads (a
  * multiple of n_heads) reads key/value head h / (n_q_heads / n_heads).  Row i of
  * a request of n rows sees the whole prefix of its group, if it has one, and its
- * agent's tokens 0 .. lens[r] - n + i (write the step's keys and values first):
+ * agent's tokens 0 .. lens[r] - n + i (write the step's keys and values first); where
+ * that is negative, the prefix alone:
  *     out = sum_c softmax_c(scale q . k_c) v_c,   lse = ln sum_c exp(scale q . k_c)
  * Tokens in units that are away are not seen; a row that sees nothing gets
  * out = 0 and lse = -infinity.  A prefix of several requests is read once for

@@ -6,7 +6,7 @@ import pytest
 from model_harness import Batch, Cache, Rows
 from oracle import model as M
 from paper_2601_21473_amd import binding as B
-from test_gpu_prefix_attention import attend, expected, run
+from test_gpu_prefix_attention import KINDS, attend, expected, run
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,16 @@ def test_fp16_weights_of_large_scores(scale):
     rng = np.random.default_rng(3)
     cache = Cache(rng, [300, 100], page=16, heads=2, dim=64, kind=M.F16, spread=2.0)
     run(cache, Batch([1, 30], [0, 1], [300, 100]), 2, M.F16, scale=scale, size=2.0)
+
+
+@pytest.mark.parametrize("kind,rows_kind", KINDS)
+@pytest.mark.parametrize("rows,lens,per", [
+    ([3, 2, 5, 1], [1, 0, 7, 1], 2), ([30, 12, 3], [5, 12, 0], 4), ([90, 70], [3, 200], 1), ([6], [2], 2)])
+@pytest.mark.parametrize("prefix", [1, 64, 150])
+def test_rows_before_their_agents_first_token(kind, rows_kind, rows, lens, per, prefix):
+    """More rows than tokens: the early ones see the prefix alone, all of it, in shared tiles
+    of a group and in requests that read the prefix for themselves."""
+    rng = np.random.default_rng(prefix)
+    n = len(rows)
+    cache = Cache(rng, lens + [prefix], page=16, heads=2, dim=64, kind=kind)
+    run(cache, Batch(rows, range(n), lens, ([0, n], [n], [prefix]), spare=1), per, rows_kind)
