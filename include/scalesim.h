@@ -534,9 +534,8 @@ ss_status ss_kv_read(const ss_kv_cache* cache, const ss_batch* batch, void* k, v
  * of a request see leaves its earlier rows of the same call unspecified.
  *   q, out     [n_rows][n_q_heads][head_dim] SS_BF16 or SS_F16 (`type`; the
  *              cache's unless that is SS_E4M3), strides in elements (multiples
- *              of 8), 16-byte aligned; out must not overlap q; n_rows * n_q_heads
- *              must be below 2^30;
- *              n_rows * n_q_heads must be below 2^30;
+ *              of 8), 16-byte aligned; out must not overlap q (from the first to
+ *              the last element of each); n_rows * n_q_heads must be below 2^30;
  *   lse        [n_rows][n_q_heads] floats, or NULL;
  *   scale      finite, also times log2(e) (1 / sqrt(head_dim) as a rule);
  *   workspace  ss_prefix_attention_workspace(...) bytes (a bound over all
@@ -580,11 +579,15 @@ typedef struct {
  * away, or have no such unit, get out = base.
  *   x [n_rows][n_in], base and out [n_rows][n_out], of the adapters' type, row
  *   strides in elements (multiples of 8), 16-byte aligned.  out may be base
- *   (same address and stride), and must not overlap x or otherwise base;
+ *   (same address and stride), and must not overlap x or otherwise base (from the
+ *   first to the last element of each);
+ *   (n_rows / 4 + n_requests) * n_out / 256 must be below 2^31;
  *   scales     [n_requests] floats or NULL;
  *   workspace  ss_adapter_add_workspace(...) bytes, 16-byte aligned, no
  *              initialisation needed.
- * A x is summed and kept in 32 bits (as two 16-bit parts in the second product). */
+ * A x is summed and kept in 32 bits (as two 16-bit parts in the second product, of
+ * fp16 with 2^-39 of the row's largest element as the least step; where an element of B
+ * is infinite, its outputs may be NaN). */
 uint64_t ss_adapter_add_workspace(const ss_adapters* adapters, uint32_t n_rows,
                                   uint32_t n_requests);
 ss_status ss_adapter_add(const ss_adapters* adapters, const ss_batch* batch, const void* x,
