@@ -452,8 +452,9 @@ struct Keys {
     // fp16 weights are held against 2^-kLift of the reference, 2^(kLift + kSlack) at most:
     // held against the reference itself those below 2^-14 of it lost bits, and those below
     // 2^-25 became nothing, which many of them together show (8,000 weights of 2^-25: the
-    // output was off by 3%).  Two powers of two stay free for the rounding of the exponents.
+    // output was off by 3%).
     static constexpr float kLift = std::is_same<P, F16>::value ? 6.f : 0.f;
+    static constexpr float kUnlift = kLift == 6.f ? 1.f / 64 : 1.f;
     // The parts of four weights.
     static __device__ __forceinline__ void weights(f32x4 e, unsigned (*w)[2]) {
         w[0][0] = P::pack(e[0], e[1]);
@@ -621,33 +622,41 @@ __device__ __forceinline__ void load_queries(const AttendArgs& A, const Item& s,
 }
 
 // Running reference and sum of one row's scores, and its weights.  `top` is an
-// unscaled score; weights are 2^(scale (score - top) + lift).
+// unscaled score; weights are 2^(scale (score - top) + lift), and sums are divided by 2^lift
+// when they are complete.
 struct Softmax {
     float top = -INFINITY, sum = 0.f;
+    float off = 0.f;            // what is added to a scaled score
+    float gate = -INFINITY;     // `top`, or -infinity in a row far from zero: every block is raised
     // Whether a score passes the reference by more than the slack (in some lane).
     __device__ bool passes(float best, float scale) const {
-        return __any(best > top && !((best - top) * scale <= kSlack));
+        return __any(best > gate && !((best - gate) * scale <= kSlack));
     }
     // Takes the largest score of the row (over the lanes that share it) as the new
-    // reference; returns what older sums shrink by.
-    __device__ float raise(float best, float scale) {
+    // reference; returns what older sums shrink by.  Score and reference are scaled and
+    // rounded apart, so the difference of equal ones is off by 2^-24 of them: of a row whose
+    // reference is beyond 2^12, it is taken from the scores themselves, block by block (for all
+    // rows that is an instruction a score more: 16 prompts 697 us, so 676 us).
+    template <int kScores>
+    __device__ float raise(float best, float scale, float lift, f32x4* scores) {
         best = fmaxf(best, __shfl_xor(best, 16));
         best = fmaxf(best, __shfl_xor(best, 32));
         best = fmaxf(best, top);
         const float shrink = top == best ? 1.f : __builtin_amdgcn_exp2f((top - best) * scale);
         top = best;
         sum *= shrink;
+        off = top == -INFINITY ? 0.f : fmaf(-top, scale, lift);
+        const bool far = fabsf(off) > 4096.f;
+        gate = far ? -INFINITY : top;
+        if (__any(far)) {
+#pragma unroll
+            for (int j = 0; j < kScores; ++j) scores[j] -= far ? top : 0.f;
+            off = far ? lift : off;
+        }
         return shrink;
     }
-    // What weights are relative to, in log2, -infinity without any score; `lift` lower than
-    // the reference itself.
-    __device__ float reference(float scale, float lift) const {
-        return top == -INFINITY ? -INFINITY : fmaf(top, scale, -lift);
-    }
-    // and what it adds to a score's exponent
-    __device__ float offset(float scale, float lift) const {
-        return top == -INFINITY ? 0.f : fmaf(-top, scale, lift);
-    }
+    // log2 of what the row's sums are relative to, -infinity without any score.
+    __device__ float reference(float scale) const { return top == -INFINITY ? -INFINITY : top * scale; }
 };
 
 // 16 rows and a range of keys.  The four waves take 64-key blocks in turn, each
@@ -783,11 +792,11 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
         for (int j = 0; j < kSub; ++j)
             best = fmaxf(fmaxf(fmaxf(best, st[j][0]), fmaxf(st[j][1], st[j][2])), st[j][3]);
         if (soft.passes(best, scale)) {
-            const float shrink = soft.raise(best, scale);
+            const float shrink = soft.template raise<kSub>(best, scale, K::kLift, st);
 #pragma unroll
             for (int c = 0; c < kCols; ++c) o[c] *= shrink;
         }
-        const float off = soft.offset(scale, K::kLift);
+        const float off = soft.off;
         unsigned w[kSub][K::kParts][2];
 #pragma unroll
         for (int j = 0; j < kSub; ++j) {
@@ -850,10 +859,10 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
             }
         }
     }
-    float sum = soft.sum;
+    float sum = soft.sum * K::kUnlift;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    const float top = soft.reference(scale, K::kLift);
+    const float top = soft.reference(scale);
 
     // join the four waves: lds_o[wave][row][kDim + 4], lds_ml[wave][row]
     constexpr int kPitch = kDim + 4;
@@ -866,7 +875,7 @@ __device__ void few_rows(const Item& s, unsigned head, char* lds) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) l += lds_ml[w * 16 + col].y * exp2f(lds_ml[w * 16 + col].x - ref);
     const bool direct = s.part == ~0ull;
-    const float mine = exp2f(top - ref) * (direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
+    const float mine = exp2f(top - ref) * K::kUnlift * (direct ? (l == 0.f ? 0.f : 1.f / l) : 1.f);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -1171,11 +1180,11 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
             for (int j = 0; j < 4; ++j)
                 best = fmaxf(fmaxf(fmaxf(best, st[t][j][0]), fmaxf(st[t][j][1], st[t][j][2])), st[t][j][3]);
             if (soft[t].passes(best, scale)) {
-                const float shrink = soft[t].raise(best, scale);
+                const float shrink = soft[t].template raise<4>(best, scale, K::kLift, st[t]);
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) o[t][c] *= shrink;
             }
-            const float off = soft[t].offset(scale, K::kLift);
+            const float off = soft[t].off;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 f32x4 e;
@@ -1218,13 +1227,13 @@ __device__ void many_rows(const Item& s, unsigned head, char* lds0, char* lds1) 
 #pragma unroll
     for (int t = 0; t < kQ; ++t) {
         const unsigned m = mw + 16 * t + col;
-        float sum = soft[t].sum;
+        float sum = soft[t].sum * K::kUnlift;
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        const float top = soft[t].reference(scale, K::kLift);
+        const float top = soft[t].reference(scale);
         if (m >= total) continue;
         const unsigned row = m / A.per, hh = head * A.per + (m - row * A.per);
-        const float mine = direct ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+        const float mine = K::kUnlift * (direct ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f);
         char* to = A.out + (u64)(s.row0 + row) * A.out_row + (u64)hh * A.out_head;
         // four columns next to each other, of one product's rows or of four products
         constexpr bool kByRow = Blocks::column(0, 1, 0) == 1;
