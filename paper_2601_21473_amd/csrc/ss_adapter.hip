@@ -445,18 +445,25 @@ void adapter_launch(const AdapterArgs& A, hipStream_t st) {
         return out_launch<T, 2>(A, st);
     }
     in_launch<T, 1>(A, st);
-    // Up to one row a request as a rule no product of 16 rows is worth its reads (256
-    // requests, 4,096 x 14,336: rank 16 38 us, as products 49 us; 32 64 and 70 us; 64 114
-    // and 156 us; eight requests 12.0 and 11.5 us).  With two rows it wins less where there
-    // are many (256 requests: rank 16 50 and 54 us, 32 82 and 75 us, 64 145 and 152 us) than
-    // it loses where there are few (eight: 13.1 and 11.3 us, 17.6 and 12.0 us, 19.8 and 14.4 us).
+    // Up to one row a request as a rule no product of 16 rows is worth its reads: bf16, 256
+    // requests, 4,096 x 14,336, an adapter each: rank 8 32 us, as products 39 us; 16 47 and
+    // 55 us; 32 79 and 80 us; 64 143 and 170 us; 128 278 and 339 us (64 requests: 16 and 18,
+    // 20 and 21, 29 and 25, 50 and 46, 87 and 86 us; eight: 11 us either way, from rank 64 on 14
+    // and 14, 18 and 20 us).  fp16 halves take a conversion each, for which registers do not
+    // suffice from rank 16 on (256 requests: rank 8 30 and 40 us, 16 76 and 55 us, 32 120 and
+    // 80 us, 64 197 and 169 us, 128 396 and 339 us), so they go this way at rank 8 only.
+    // With two rows a request it wins less where there are many (bf16, 256 requests: rank 16
+    // 50 and 54 us, 32 82 and 75 us, 64 145 and 152 us) than it loses where there are few
+    // (eight: 13.1 and 11.3 us, 17.6 and 12.0 us, 19.8 and 14.4 us).
     if (A.n_rows <= A.n_requests) {
-        switch (A.rank) {
-            case 8: return out_few_launch<T, 1>(A, st);
-            case 16: return out_few_launch<T, 2>(A, st);
-            case 32: return out_few_launch<T, 4>(A, st);
-            case 64: return out_few_launch<T, 8>(A, st);
-            case 128: return out_few_launch<T, 16>(A, st);
+        if (A.rank == 8) return out_few_launch<T, 1>(A, st);
+        if constexpr (std::is_same<T, Bf16>::value) {
+            switch (A.rank) {
+                case 16: return out_few_launch<T, 2>(A, st);
+                case 32: return out_few_launch<T, 4>(A, st);
+                case 64: return out_few_launch<T, 8>(A, st);
+                case 128: return out_few_launch<T, 16>(A, st);
+            }
         }
     }
     out_launch<T, 1>(A, st);
