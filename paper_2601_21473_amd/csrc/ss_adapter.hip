@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kThreads, kSub == 1 ? 3 : 2) void k_adapter_out(Ada
     }
 }
 
-// Decoding: a workgroup per tile of up to four rows and A.cols columns.  With so few rows
+// Decoding in bf16, and at rank 8: a workgroup per tile of up to four rows and A.cols columns.  With so few rows
 // B's bytes bound it, so they are read as they lie, 16 bytes a lane, and multiplied in
 // 32 bits: a column's ranks are in kSplit = rank / 8 lanes next to each other, each of
 // which takes eight columns in a row, so that the sums need log2(kSplit) exchanges and
